@@ -33,6 +33,9 @@ extern "C" {
 #define SPEC_MAX_HEADS 8     /* stages of the speculator (the paper uses 3, 5 and 7)         */
 #define SPEC_MAX_TOPK 8      /* branching factor of one head                                  */
 #define SPEC_MAX_LEAVES 4096 /* product of the branching factors, per sequence                */
+#define SPEC_MAX_TREE_NODES 1024   /* nodes of one sequence's tree of drafted tokens            */
+#define SPEC_MAX_TREE_DEPTH 64     /* tokens of one candidate that is merged into a tree        */
+#define SPEC_MAX_TREE_ENTRIES 8192 /* K * n of the candidates of one tree                       */
 
 enum spec_status {
     SPEC_OK = 0,
@@ -46,11 +49,14 @@ enum spec_status {
     SPEC_ERR_NO_DEVICE = 7,   /* no CUDA device / not an sm_100 part                          */
     SPEC_ERR_STATIC_SCRATCH = 8, /* spec_verify_static: the problem needs more scratch than the
                                  built-in array holds (SPEC_VERIFY_STATIC_SCRATCH_BYTES)      */
-    SPEC_ERR_INDEX_RANGE = 9  /* device: spec_next_ctx met best_cand outside [0, K) or accept_len
-                                 outside [0, n] (that sequence's row is written as zeros)     */
+    SPEC_ERR_INDEX_RANGE = 9, /* device: spec_next_ctx met best_cand outside [0, K) or accept_len
+                                 outside [0, n] (that sequence's row is written as zeros); a length, page,
+                                 node or slot of a paged cache was out of range (see the calls)  */
+    SPEC_ERR_PAGES = 10       /* device: spec_page_tables ran out of free pages or of a row's entries */
 };
 
-enum spec_dtype { SPEC_BF16 = 0, SPEC_F32 = 1 };
+/* SPEC_F16 is taken by spec_tree_attention and spec_verify_tree */
+enum spec_dtype { SPEC_BF16 = 0, SPEC_F32 = 1, SPEC_F16 = 2 };
 
 enum spec_option {
     SPEC_OPT_GEMM_IMPL = 0,    /* 0 (default): tcgen05/TMEM tensor-core kernels; 1: slow CUDA-core
@@ -311,6 +317,147 @@ int spec_draft_vp_merge(spec_handle_t h, int level, int B, const int32_t *topk, 
  */
 int spec_quantize_head(spec_handle_t h, int level, void *q_out, float *scale_out, void *cuda_stream);
 int spec_set_head_fp8(spec_handle_t h, int level, const void *q, const float *scale);
+
+/* ==== the base model's forward pass over a tree of drafted tokens ==============================
+ * Between spec_draft and the acceptance of its tokens a serving program runs its base model once over all candidates.
+ * (Sec. 3.1 of the paper has the base model attend to a tree of candidates, so that shared prefixes are computed once.)  The calls
+ * below are the device work around and inside that pass which is not a plain matrix product:
+ *     spec_tree_plan       the K candidates of a sequence become one tree of T nodes, shared prefixes once
+ *     spec_page_tables     the block tables of a paged cache grow for the tokens to come; the slot of each
+ *     spec_tree_attention  per layer: the tree's queries attend to the cache and to their ancestors in the tree
+ *     spec_verify_tree     the accepted path of the tree by the base model's logits, the next token behind it
+ *     spec_kv_commit       the accepted path's keys and values, all layers, go to their slots in the cache
+ * then spec_next_ctx on base_state seen as [B, 1, T, d_base] with best_cand = 0 and accept_len = last_node, and spec_draft.
+ * All of them only enqueue kernels on `cuda_stream`, with the device that owns the pointers current.  `err_word` (dev
+ * int32, or NULL) receives the first device-side error if it was 0; it is never cleared here, and spec_poll_error
+ * reads it.  Strides are in elements; a dimension of size 1 may have stride 0.
+ *
+ * ---- spec_tree_plan: candidates to tree
+ *   cand_tok  dev int32 [B, K, n]   candidates, best first (spec_draft's); a negative token ends its candidate
+ *   last_tok  dev int32 [B]         the token the candidates follow: the tree's root, node 0
+ *   seq_len   dev int32 [B]         tokens in the cache: the root's position
+ *   T         nodes per sequence in the outputs.  Node numbers follow the candidates in order (a node is numbered when the first
+ *             candidate reaches it, so parents precede children); nodes numbered T or more are left out.
+ *   tok, pos, parent  dev int32 [B, T] (out)  token, position seq_len + depth, parent node (-1 for the root)
+ *   mask      dev uint32 [B, T, ceil(T / 32)] (out)  bit t % 32 of word t / 32: node t is the node itself or an ancestor
+ *   node_of   dev int32 [B, K, n + 1] (out)   node of every candidate's position, [.., 0] = 0 (the root); -1: left out
+ *   n_nodes   dev int32 [B] (out)             nodes in use, 1 .. T
+ * Rows behind a sequence's nodes get token 0, position seq_len, parent -1 and an empty mask.
+ * Limits: T <= SPEC_MAX_TREE_NODES, n <= SPEC_MAX_TREE_DEPTH, K <= SPEC_MAX_LEAVES, K * n <= SPEC_MAX_TREE_ENTRIES; else
+ * SPEC_ERR_SHAPE. */
+int spec_tree_plan(const int32_t *cand_tok, const int32_t *last_tok, const int32_t *seq_len, int B, int K, int n, int T,
+                   int32_t *tok, int32_t *pos, int32_t *parent, uint32_t *mask, int32_t *node_of, int32_t *n_nodes,
+                   void *cuda_stream);
+
+/* ---- spec_page_tables: block tables and slots from lengths
+ * Sequence b holds n_pages[b] pages, block_table[b, 0 .. n_pages[b]), and wants room for seq_len[b] + n_new[b] tokens.  The pages
+ * that it lacks are taken from the end of free_pages, in order of the sequences: with `before` pages dealt to earlier sequences
+ * its i-th new page is free_pages[*free_count - 1 - before - i].  Pages are never taken away.
+ *   seq_len      dev int32 [B];  n_new  dev int32 [B] in [0, max_new], or NULL: max_new everywhere
+ *   block_table  dev int32 [B, max_pages], rows table_stride elements apart (in / out)
+ *   n_pages, free_count  dev int32 [B], [1];  free_pages  dev int32 [n_free]
+ *   slots        dev int64 [B, max_new] (out)  page * page_size + offset of position seq_len + j, -1 for j >= n_new
+ *   n_pages_out, free_count_out  dev int32 [B], [1] (out); may be n_pages and free_count themselves
+ * When pages run short, the first sequence that does not get all it lacks gets none, nor do later ones that lack any; neither does
+ * one whose row is too short (it takes nothing from the others).  Slots behind the pages that a sequence holds are -1
+ * and err_word receives SPEC_ERR_PAGES.  Lengths and counts out of range are clamped, a negative page id gives slot -1, and
+ * err_word receives SPEC_ERR_INDEX_RANGE. */
+int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int page_size, int max_new, int32_t *block_table,
+                     int64_t table_stride, int max_pages, const int32_t *n_pages, const int32_t *free_pages,
+                     const int32_t *free_count, int n_free, int64_t *slots, int32_t *n_pages_out, int32_t *free_count_out,
+                     int32_t *err_word, void *cuda_stream);
+
+/* ---- spec_tree_attention: a tree's queries over a paged cache and the tree itself
+ * For node i < n_nodes[b] and query head h (key head g = h / (Hq / Hkv)), over the keys
+ *     cache positions 0 .. seq_len[b]-1 of head g, and the tree's nodes t < n_nodes[b] whose bit is set in mask[b, i]:
+ *     out[b, i, h] = sum softmax(scale * <q[b, i, h], key>) * value,   lse[b, i, h] = log sum exp(scale * <q, key>)
+ * A row without any key gets zeros and lse = -inf.  Keys that a row does not see do not touch it, whatever they hold.  Rows
+ * i >= n_nodes[b] of out and lse are left as they are.  T = 1 without a mask is a plain decoding step.
+ * Scores, softmax statistics and sums are fp32; the probabilities are rounded to `dtype` before they meet the values.
+ *   dtype        SPEC_BF16 or SPEC_F16, of q, k, v, caches and out; 16-byte aligned pointers, strides multiples of 8
+ *   q, out       dev [B, T, Hq, D], strides (sequence, node, head);  k, v  dev [B, T, Hkv, D], the same
+ *   k_cache, v_cache  dev [n_pages, page_size, Hkv, D], strides (page, token, head): any order of these in memory
+ *   block_table  dev int32 [B, max_pages], rows table_stride apart: page of positions j * page_size ..
+ *   n_nodes      dev int32 [B], or NULL: T everywhere
+ *   mask         dev uint32 [B, T, ceil(T / 32)] as spec_tree_plan writes it, or NULL: node i sees nodes 0 .. i (a chain)
+ *   lse          dev fp32 [B, T, Hq], or NULL
+ *   workspace    dev, 256-byte aligned, >= spec_tree_attention_workspace_bytes(...); need not be zeroed.  Calls that may
+ *                overlap on the GPU need workspaces of their own.
+ * Limits: D a multiple of 8, at most 128; Hq a multiple of Hkv; T <= SPEC_MAX_TREE_NODES; else SPEC_ERR_SHAPE.
+ * Lengths out of [0, max_pages * page_size] and node counts out of [0, T] are clamped, a page id outside [0, n_pages) reads as
+ * zeros, and err_word receives SPEC_ERR_INDEX_RANGE. */
+typedef struct {
+    int32_t dtype, B, T, Hq, Hkv, D;
+    int32_t page_size, n_pages, max_pages;
+    float scale;
+    const void *q, *k, *v, *k_cache, *v_cache;
+    const int32_t *block_table, *seq_len, *n_nodes;
+    const uint32_t *mask;
+    void *out;
+    float *lse;
+    int32_t *err_word;
+    int64_t table_stride;
+    int64_t q_stride[3], k_stride[3], v_stride[3], kc_stride[3], vc_stride[3], out_stride[3];
+} spec_tree_attention_t;
+size_t spec_tree_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D);
+int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ---- spec_verify_tree: the accepted path
+ * From the root on: g = first index of the maximum of the node's logits (NaN never wins); the walk goes on to the child that
+ * carries token g (the lowest, if several do), and ends where there is none, or behind n of them.
+ * With constraints the maximum is that of the adjusted logits of the allowed tokens, computed in fp32 in this order:
+ *     x = x > 0 ? x / repetition : x * repetition   for tokens in the history or taken on the walk so far
+ *     x = x - frequency * c - presence              for tokens generated c > 0 times: in the history behind the prompt, or on the walk
+ *     x = x + bias                                  for tokens in the bias list (a token's last entry counts)
+ * A row that allows nothing gives g = -1.  Only the rows on the path are read.
+ *   tok, parent, n_nodes  dev int32 [B, T], [B, T], [B]   the tree (spec_tree_plan); parents precede their children
+ *   logits       dev [B, T, V] of logits_dtype (SPEC_BF16, SPEC_F16, SPEC_F32), strides (sequence, node)
+ *   n            longest path, 0 <= n <= SPEC_MAX_TREE_DEPTH
+ *   hist_tok, hist_len  dev int32 [B, max_hist], [B]   prompt and generated tokens of each sequence, the root's among them; NULL:
+ *                no penalties.  prompt_len dev int32 [B]: how many of them are prompt (NULL: none)
+ *   repetition, frequency, presence  dev fp32 [B], or NULL: 1, 0, 0
+ *   bias_tok, bias_val, bias_len  dev int32 / fp32 [B, max_bias], int32 [B] (NULL: max_bias); bias_tok NULL: no biases
+ *   allow        dev uint32 [B, T, ceil(V / 32)], bit set: the token is allowed; NULL: all are
+ *   accept_len, last_node, next_tok  dev int32 [B] (out)   tokens accepted, last node of the path, g behind it
+ *   path         dev int32 [B, n + 1] (out)   nodes of the path, path[.., 0] = 0; -1 behind it
+ * List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 gets accept_len 0 and -1 elsewhere. */
+typedef struct {
+    int32_t logits_dtype, B, T, V, n, max_hist, max_bias;
+    const int32_t *tok, *parent, *n_nodes;
+    const void *logits;
+    int64_t logits_stride[2];
+    const int32_t *hist_tok, *hist_len, *prompt_len;
+    const float *repetition, *frequency, *presence;
+    const int32_t *bias_tok;
+    const float *bias_val;
+    const int32_t *bias_len;
+    const uint32_t *allow;
+    int32_t *accept_len, *last_node, *next_tok, *path;
+} spec_tree_verify_t;
+int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
+
+/* ---- spec_kv_commit: the accepted path's keys and values
+ *     k_cache[l, page, offset] = k[l, b, path[b, j]],  v likewise,  for j = 0 .. accept_len[b], slots[b, j] = (page, offset)
+ *     new_len[b] = seq_len[b] + accept_len[b] + 1
+ * for all L layers in one launch.  16-bit elements of any type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
+ *   k, v         dev [L, B, T, H, D], strides (layer, sequence, node, head)
+ *   k_cache, v_cache  dev [L, n_pages, page_size, H, D], strides (layer, page, token, head)
+ *   path         dev int32 [B, n + 1], accept_len dev int32 [B]   as spec_verify_tree writes them
+ *   slots        dev int64 [B, n + 1]   as spec_page_tables writes them for max_new = n + 1
+ *   seq_len, new_len  dev int32 [B]; new_len may be seq_len, or NULL
+ * accept_len beyond n is taken as n, below 0 nothing is copied.  A node outside [0, T) or a slot outside the cache is not copied, and
+ * err_word receives SPEC_ERR_INDEX_RANGE. */
+typedef struct {
+    int32_t L, B, T, n, H, D, page_size, n_pages;
+    const void *k, *v;
+    void *k_cache, *v_cache;
+    const int32_t *path, *accept_len;
+    const int64_t *slots;
+    const int32_t *seq_len;
+    int32_t *new_len, *err_word;
+    int64_t k_stride[4], v_stride[4], kc_stride[4], vc_stride[4];
+} spec_kv_commit_t;
+int spec_kv_commit(const spec_kv_commit_t *c /*host*/, void *cuda_stream);
 
 /* Per-kernel device times of the last spec_draft issued with SPEC_OPT_PROFILE = 1, in launch
  * order: for every head (projection GEMM, mix/LayerNorm/GELU, head GEMM, merge/expand), then

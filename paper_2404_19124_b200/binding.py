@@ -9,7 +9,8 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
-from typing import Tuple, List, Optional, Sequence
+import struct
+from typing import NamedTuple, Tuple, List, Optional, Sequence
 
 import torch
 
@@ -18,9 +19,10 @@ LIB_PATH = os.path.join(_PKG, "libspec_b200.so")
 
 MAX_HEADS, MAX_TOPK, MAX_LEAVES = 8, 8, 4096
 (SPEC_OK, SPEC_ERR_INVALID_ARG, SPEC_ERR_SHAPE, SPEC_ERR_WORKSPACE, SPEC_ERR_CUDA, SPEC_ERR_TOKEN_RANGE,
- SPEC_ERR_TIMEOUT, SPEC_ERR_NO_DEVICE, SPEC_ERR_STATIC_SCRATCH, SPEC_ERR_INDEX_RANGE) = range(10)
+ SPEC_ERR_TIMEOUT, SPEC_ERR_NO_DEVICE, SPEC_ERR_STATIC_SCRATCH, SPEC_ERR_INDEX_RANGE, SPEC_ERR_PAGES) = range(11)
 SPEC_VERIFY_STATIC_SCRATCH_BYTES = 1 << 20
-SPEC_BF16, SPEC_F32 = 0, 1
+SPEC_BF16, SPEC_F32, SPEC_F16 = 0, 1, 2
+MAX_TREE_NODES, MAX_TREE_DEPTH, MAX_TREE_ENTRIES = 1024, 64, 8192
 SPEC_OPT_GEMM_IMPL, SPEC_OPT_HEAD_BLOCK_N, SPEC_OPT_PROJ_BLOCK_N, SPEC_OPT_PROFILE, SPEC_OPT_FP8_MAX_ROWS = 0, 1, 2, 3, 4
 SPEC_OPT_HEAD_SWAP_MAX_ROWS = 5
 SPEC_OPT_GEMM_PRODUCERS = 6
@@ -33,6 +35,8 @@ EXPORTS = [
     "spec_verify_static", "spec_verify_early", "spec_quantize_head", "spec_set_head_fp8",
     "spec_head_partials", "spec_next_ctx", "spec_choose_k",
     "spec_set_vocab_shard", "spec_draft_vp_exchange", "spec_draft_vp_local", "spec_draft_vp_merge",
+    "spec_tree_plan", "spec_page_tables", "spec_tree_attention_workspace_bytes", "spec_tree_attention", "spec_verify_tree",
+    "spec_kv_commit",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -102,6 +106,14 @@ _lib.spec_head_logits.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_
 _lib.spec_head_partials.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.spec_head_topk.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                 C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.spec_tree_plan.argtypes = [C.c_void_p] * 3 + [C.c_int] * 4 + [C.c_void_p] * 7
+_lib.spec_page_tables.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 5
+_lib.spec_tree_attention_workspace_bytes.restype = C.c_size_t
+_lib.spec_tree_attention_workspace_bytes.argtypes = [C.c_int] * 5
+_lib.spec_tree_attention.argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.spec_verify_tree.argtypes = [C.c_char_p, C.c_void_p]
+_lib.spec_kv_commit.argtypes = [C.c_char_p, C.c_void_p]
 
 class SpecError(RuntimeError):
     def __init__(self, status: int, where: str):
@@ -445,6 +457,242 @@ def spec_next_ctx(base_state: torch.Tensor, best_cand: torch.Tensor, accept_len:
             status = _lib.spec_next_ctx(*args, _stream_ptr(stream))
     _check(status, "spec_next_ctx")
     return ctx_state
+
+
+# ---- the base model's forward pass over a tree of drafted tokens ------------------------------------------------------
+class SpecTree(NamedTuple):
+    """What spec_tree_plan writes, all int32: tok, pos, parent [B, T], mask [B, T, ceil(T / 32)] (bit words), node_of
+    [B, K, n + 1], n_nodes [B]."""
+    tok: torch.Tensor
+    pos: torch.Tensor
+    parent: torch.Tensor
+    mask: torch.Tensor
+    node_of: torch.Tensor
+    n_nodes: torch.Tensor
+
+
+def _on(t: Optional[torch.Tensor], device: torch.device, dtype: torch.dtype, shape, name: str):
+    """Address of a contiguous tensor of that type, shape and device; None stays None."""
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _strided(t: torch.Tensor, device: torch.device, dtype: torch.dtype, shape, name: str, written: bool = False):
+    """Strides of all dimensions but the last, which has to be dense; 0 where a dimension has one entry."""
+    if t.device != device or t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{name}: the last dimension must be dense")
+    stride = [0 if n == 1 else s for n, s in zip(shape[:-1], stride)]
+    if written and any(s == 0 and n > 1 for n, s in zip(shape, stride)):
+        raise ValueError(f"{name} is written and must not be expanded")
+    return stride
+
+
+def _cuda_device(t: torch.Tensor, name: str) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.device
+
+
+def _made(t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device,
+          stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """`t`, or a new tensor that belongs to the stream the call runs on."""
+    if t is not None:
+        return t
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _launch(device: torch.device, where: str, fn, *args, stream: Optional[torch.cuda.Stream]) -> None:
+    """Calls fn(*args, stream) with `device` current."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream belongs to {stream.device}, the tensors to {device}")
+    if _current_device is not None and device.index == _current_device():
+        status = fn(*args, _stream_ptr(stream))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _stream_ptr(stream))
+    if status != SPEC_OK:
+        raise SpecError(status, where)
+
+
+def _err_ptr(err_workspace: Optional[torch.Tensor], device: torch.device):
+    if err_workspace is None:
+        return None
+    if err_workspace.device != device or err_workspace.data_ptr() % 4 or err_workspace.numel() * err_workspace.element_size() < 4:
+        raise ValueError(f"err_workspace must hold an int32 word on {device}")
+    return err_workspace.data_ptr()
+
+
+def spec_tree_plan(cand_tok: torch.Tensor, last_tok: torch.Tensor, seq_len: torch.Tensor, T: int,
+                   tree: Optional[SpecTree] = None, stream: Optional[torch.cuda.Stream] = None) -> SpecTree:
+    """The candidates [B, K, n] of every sequence as one tree of at most T nodes, shared prefixes once."""
+    dev = _cuda_device(cand_tok, "cand_tok")
+    B, K, n = cand_tok.shape
+    T = int(T)
+    if T < 1:
+        raise SpecError(SPEC_ERR_INVALID_ARG, "spec_tree_plan")
+    i32, W = torch.int32, (T + 31) // 32
+    cand, last, lens = (_on(cand_tok, dev, i32, (B, K, n), "cand_tok"), _on(last_tok, dev, i32, (B,), "last_tok"),
+                        _on(seq_len, dev, i32, (B,), "seq_len"))
+    shapes = ((B, T), (B, T), (B, T), (B, T, W), (B, K, n + 1), (B,))
+    tree = SpecTree(*(_made(None if tree is None else tree[i], s, i32, dev, stream) for i, s in enumerate(shapes)))
+    out = [_on(t, dev, i32, s, name) for t, s, name in zip(tree, shapes, SpecTree._fields)]
+    _launch(dev, "spec_tree_plan", _lib.spec_tree_plan, cand, last, lens, B, K, n, T, *out, stream=stream)
+    return tree
+
+
+def spec_page_tables(seq_len: torch.Tensor, n_new: Optional[torch.Tensor], block_table: torch.Tensor, n_pages: torch.Tensor,
+                     free_pages: torch.Tensor, free_count: torch.Tensor, page_size: int, max_new: Optional[int] = None,
+                     slots: Optional[torch.Tensor] = None, n_pages_out: Optional[torch.Tensor] = None,
+                     free_count_out: Optional[torch.Tensor] = None, err_workspace: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Grows block_table [B, max_pages] for seq_len + n_new tokens (n_new None: max_new everywhere) from the end of free_pages;
+    returns slots, int64 [B, max_new].  n_pages [B] and free_count [1] are updated in place unless outputs for them are given."""
+    dev = _cuda_device(seq_len, "seq_len")
+    i32, (B,) = torch.int32, seq_len.shape
+    if max_new is None:
+        if slots is None:
+            raise ValueError("give max_new or slots")
+        max_new = slots.shape[1]
+    slots = _made(slots, (B, max_new), torch.int64, dev, stream)
+    max_pages = block_table.shape[1]
+    stride = _strided(block_table, dev, i32, (B, max_pages), "block_table", written=True)[0]
+    n_pages_out = n_pages if n_pages_out is None else n_pages_out
+    free_count_out = free_count if free_count_out is None else free_count_out
+    _launch(dev, "spec_page_tables", _lib.spec_page_tables, _on(seq_len, dev, i32, (B,), "seq_len"),
+            _on(n_new, dev, i32, (B,), "n_new"), B, int(page_size), int(max_new), block_table.data_ptr(), stride or max_pages,
+            max_pages, _on(n_pages, dev, i32, (B,), "n_pages"),
+            _on(free_pages, dev, i32, (free_pages.numel(),), "free_pages"), _on(free_count, dev, i32, (1,), "free_count"),
+            free_pages.numel(), _on(slots, dev, torch.int64, (B, max_new), "slots"),
+            _on(n_pages_out, dev, i32, (B,), "n_pages_out"), _on(free_count_out, dev, i32, (1,), "free_count_out"),
+            _err_ptr(err_workspace, dev), stream=stream)
+    return slots
+
+
+_DTYPES = {torch.bfloat16: SPEC_BF16, torch.float32: SPEC_F32, torch.float16: SPEC_F16}
+# spec_tree_attention_t, spec_tree_verify_t and spec_kv_commit_t; null pointers are 0
+_ATTENTION = struct.Struct("@9if12P19q")
+_TREE_VERIFY = struct.Struct("@7i4P2q14P")
+_COMMIT = struct.Struct("@8i10P16q")
+
+
+def spec_tree_attention_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(_lib.spec_tree_attention_workspace_bytes(int(B), int(T), int(Hq), int(Hkv), int(D)))
+
+
+def spec_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                        block_table: torch.Tensor, seq_len: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                        n_nodes: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, err_workspace: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """q [B, T, Hq, D] over the cache [pages, page_size, Hkv, D] (any strides but a dense last dimension; a cache kept as
+    [pages, Hkv, page_size, D] is passed transposed) and the tree's own k, v [B, T, Hkv, D].  mask: SpecTree.mask, None for
+    chains; scale: D ** -0.5 by default.  Returns out; lse (fp32 [B, T, Hq]) is written when given."""
+    dev = _cuda_device(q, "q")
+    dt, i32 = q.dtype, torch.int32
+    if dt != torch.bfloat16 and dt != torch.float16:
+        raise ValueError("q must be bf16 or fp16")
+    B, T, Hq, D = q.shape
+    Hkv = k.shape[2]
+    pages, page_size = k_cache.shape[:2]
+    max_pages = block_table.shape[1]
+    made = out is None
+    out = _made(out, (B, T, Hq, D), dt, dev, stream)
+    if workspace is None:
+        need = spec_tree_attention_workspace_bytes(B, T, Hq, Hkv, D)
+        if need == 0:
+            raise SpecError(SPEC_ERR_SHAPE, "spec_tree_attention_workspace_bytes")
+        workspace = _made(None, (need,), torch.uint8, dev, stream)
+    elif workspace.device != dev:
+        raise ValueError(f"workspace must be on {dev}")
+    rows, cache = (B, T, Hkv, D), (pages, page_size, Hkv, D)
+    strides = (_strided(q, dev, dt, (B, T, Hq, D), "q") + _strided(k, dev, dt, rows, "k") + _strided(v, dev, dt, rows, "v") +
+               _strided(k_cache, dev, dt, cache, "k_cache") + _strided(v_cache, dev, dt, cache, "v_cache") +
+               _strided(out, dev, dt, (B, T, Hq, D), "out", written=True))
+    table_stride = _strided(block_table, dev, i32, (B, max_pages), "block_table")[0] if B > 1 else max_pages
+    args = _ATTENTION.pack(
+        _DTYPES[dt], B, T, Hq, Hkv, D, page_size, pages, max_pages, D ** -0.5 if scale is None else scale, q.data_ptr(),
+        k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
+        _on(seq_len, dev, i32, (B,), "seq_len"), _on(n_nodes, dev, i32, (B,), "n_nodes") or 0,
+        _on(mask, dev, i32, (B, T, (T + 31) // 32), "mask") or 0, out.data_ptr(),
+        _on(lse, dev, torch.float32, (B, T, Hq), "lse") or 0, _err_ptr(err_workspace, dev) or 0, table_stride, *strides)
+    _launch(dev, "spec_tree_attention", _lib.spec_tree_attention, args, workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), stream=stream)
+    return out
+
+
+def spec_verify_tree(tok: torch.Tensor, parent: torch.Tensor, n_nodes: torch.Tensor, logits: torch.Tensor,
+                     n: Optional[int] = None, hist_tok: Optional[torch.Tensor] = None, hist_len: Optional[torch.Tensor] = None,
+                     prompt_len: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                     frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                     bias_tok: Optional[torch.Tensor] = None, bias_val: Optional[torch.Tensor] = None,
+                     bias_len: Optional[torch.Tensor] = None, allow: Optional[torch.Tensor] = None,
+                     accept_len: Optional[torch.Tensor] = None, last_node: Optional[torch.Tensor] = None,
+                     next_tok: Optional[torch.Tensor] = None, path: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None):
+    """Greedy walk down the trees by logits [B, T, V] (bf16, fp16 or fp32; a dense last dimension), at most n tokens deep (n
+    None: as long as path).  Returns (accept_len, last_node, next_tok, path).  Penalties need hist_tok and hist_len."""
+    dev = _cuda_device(logits, "logits")
+    i32, f32 = torch.int32, torch.float32
+    if logits.dtype not in _DTYPES:
+        raise ValueError("logits must be bf16, fp16 or fp32")
+    B, T, V = logits.shape
+    if n is None:
+        if path is None:
+            raise ValueError("give n or path")
+        n = path.shape[1] - 1
+    accept_len, last_node, next_tok = (_made(t, (B,), i32, dev, stream) for t in (accept_len, last_node, next_tok))
+    path = _made(path, (B, n + 1), i32, dev, stream)
+    max_hist = 0 if hist_tok is None else hist_tok.shape[1]
+    max_bias = 0 if bias_tok is None else bias_tok.shape[1]
+    vec = lambda t, dt, name: _on(t, dev, dt, (B,), name) or 0
+    args = _TREE_VERIFY.pack(
+        _DTYPES[logits.dtype], B, T, V, n, max_hist, max_bias, _on(tok, dev, i32, (B, T), "tok"),
+        _on(parent, dev, i32, (B, T), "parent"), _on(n_nodes, dev, i32, (B,), "n_nodes"), logits.data_ptr(),
+        *_strided(logits, dev, logits.dtype, (B, T, V), "logits"), _on(hist_tok, dev, i32, (B, max_hist), "hist_tok") or 0,
+        vec(hist_len, i32, "hist_len"), vec(prompt_len, i32, "prompt_len"), vec(repetition, f32, "repetition"),
+        vec(frequency, f32, "frequency"), vec(presence, f32, "presence"), _on(bias_tok, dev, i32, (B, max_bias), "bias_tok") or 0,
+        _on(bias_val, dev, f32, (B, max_bias), "bias_val") or 0, vec(bias_len, i32, "bias_len"),
+        _on(allow, dev, i32, (B, T, (V + 31) // 32), "allow") or 0, _on(accept_len, dev, i32, (B,), "accept_len"),
+        _on(last_node, dev, i32, (B,), "last_node"), _on(next_tok, dev, i32, (B,), "next_tok"),
+        _on(path, dev, i32, (B, n + 1), "path"))
+    _launch(dev, "spec_verify_tree", _lib.spec_verify_tree, args, stream=stream)
+    return accept_len, last_node, next_tok, path
+
+
+def spec_kv_commit(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, path: torch.Tensor,
+                   accept_len: torch.Tensor, slots: torch.Tensor, seq_len: Optional[torch.Tensor] = None,
+                   new_len: Optional[torch.Tensor] = None, err_workspace: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Copies the accepted path's rows of k, v [L, B, T, H, D] to the slots [B, n + 1] of the caches [L, pages, page_size, H, D];
+    new_len (may be seq_len) receives seq_len + accept_len + 1."""
+    dev = _cuda_device(k, "k")
+    dt, i32 = k.dtype, torch.int32
+    if dt.itemsize != 2:
+        raise ValueError("keys and values must have 16-bit elements")
+    L, B, T, H, D = k.shape
+    pages, page_size = k_cache.shape[1:3]
+    n1 = path.shape[1]
+    cache = (L, pages, page_size, H, D)
+    strides = (_strided(k, dev, dt, (L, B, T, H, D), "k") + _strided(v, dev, dt, (L, B, T, H, D), "v") +
+               _strided(k_cache, dev, dt, cache, "k_cache", written=True) +
+               _strided(v_cache, dev, dt, cache, "v_cache", written=True))
+    args = _COMMIT.pack(L, B, T, n1 - 1, H, D, page_size, pages, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(),
+                        v_cache.data_ptr(), _on(path, dev, i32, (B, n1), "path"), _on(accept_len, dev, i32, (B,), "accept_len"),
+                        _on(slots, dev, torch.int64, (B, n1), "slots"), _on(seq_len, dev, i32, (B,), "seq_len") or 0,
+                        _on(new_len, dev, i32, (B,), "new_len") or 0, _err_ptr(err_workspace, dev) or 0, *strides)
+    _launch(dev, "spec_kv_commit", _lib.spec_kv_commit, args, stream=stream)
 
 
 def spec_attach_fp8_heads(h: SpecHandle, levels: Optional[Sequence[int]] = None,

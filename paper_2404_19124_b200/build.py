@@ -17,7 +17,7 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libspec_b200.so")
 PYCALL_PATH = os.path.join(_PKG, "_pycall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["spec_api.cu", "verify_kernels.cu", "draft_kernels.cu", "draft_small.cu", "fp8_kernels.cu", "gemm_tcgen05.cu",
-           "gemm_pair.cu", "gemm_simt.cu"]
+           "gemm_pair.cu", "gemm_simt.cu", "tree_steps.cu", "tree_attention.cu"]
 
 
 def _newest_source_mtime() -> float:

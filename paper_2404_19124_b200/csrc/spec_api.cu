@@ -379,7 +379,8 @@ const char *spec_status_str(int s) {
         case SPEC_ERR_TIMEOUT: return "bounded wait inside a kernel ran out";
         case SPEC_ERR_NO_DEVICE: return "no usable CUDA device";
         case SPEC_ERR_STATIC_SCRATCH: return "problem needs more scratch than the library's built-in array holds";
-        case SPEC_ERR_INDEX_RANGE: return "device: best_cand or accept_len out of range in spec_next_ctx";
+        case SPEC_ERR_INDEX_RANGE: return "device: an index, length or page id was out of range";
+        case SPEC_ERR_PAGES: return "device: not enough free pages, or a block table's row is too short";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,617 @@
+// What a serving program does around the base model's forward pass over a tree of drafted tokens, apart from the attention
+// (tree_attention.cu): merging the candidates into the tree, block tables and slots of a paged cache, the greedy walk
+// down the tree's logits, and the copy of the accepted keys and values to the cache (Sec. 3.1, Sec. 4.1 of arXiv 2404.19124
+// describe the tree; the cache and the constraints are the serving program's).
+#include <limits.h>
+#include <math.h>
+
+#include <cuda_fp16.h>
+
+#include "spec_common.cuh"
+
+namespace spec {
+
+namespace {
+
+__device__ __forceinline__ int warp_inclusive_sum(int x) {
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if ((threadIdx.x & 31) >= off) x += y;
+    }
+    return x;
+}
+
+// Inclusive sum over the block's threads; `total` receives the whole.  `part`: 33 ints of shared memory.
+__device__ int block_inclusive_sum(int x, int *part, int &total) {
+    const int warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
+    x = warp_inclusive_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 31) part[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        const int mine = threadIdx.x < warps ? part[threadIdx.x] : 0;
+        const int sum = warp_inclusive_sum(mine);
+        part[threadIdx.x] = sum - mine;
+        if (threadIdx.x == 31) part[32] = sum;
+    }
+    __syncthreads();
+    total = part[32];
+    return x + part[warp];
+}
+
+// ---- the candidates' tree ------------------------------------------------------------------------------------------
+// One CTA per sequence.  Level by level, candidates with the same first j + 1 tokens find each other through a hash table in
+// shared memory whose entries keep the lowest of them (a table of pairs (lowest candidate with the same j tokens, token)); an entry
+// (k, j) whose lowest candidate is k itself is a new node, and its number is its rank in (k, j) order, a prefix sum.
+// All of it is latency: 2 n + 6 barriers.
+constexpr int kPlanMaxThreads = 1024;
+
+struct PlanSmem {            // offsets in bytes
+    int keys, low, first, number, parent, total;
+    int slots;               // of the hash table, a power of two
+};
+__host__ __device__ inline PlanSmem plan_smem(int K, int n, int T) {
+    PlanSmem s;
+    s.slots = 32;
+    while (s.slots < 2 * K) s.slots *= 2;
+    s.keys = 0;
+    s.low = s.slots * 8;
+    s.first = s.low + s.slots * 4;          // [K, n] lowest candidate with the same prefix, -1 behind the end
+    s.number = s.first + K * n * 4;         // [K, n] number of a new node
+    s.parent = s.number + K * n * 4;        // [T]
+    s.total = s.parent + T * 4;
+    return s;
+}
+
+__global__ void __launch_bounds__(kPlanMaxThreads)
+tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *seq_len, int K, int n, int T, int32_t *tok,
+                 int32_t *pos, int32_t *parent, uint32_t *mask, int32_t *node_of, int32_t *n_nodes) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int part[33];
+    griddep_launch();
+    griddep_wait();
+    const PlanSmem lay = plan_smem(K, n, T);
+    unsigned long long *keys = (unsigned long long *)(smem + lay.keys);
+    int *low = (int *)(smem + lay.low), *first = (int *)(smem + lay.first), *number = (int *)(smem + lay.number);
+    int *up = (int *)(smem + lay.parent);
+    const int b = blockIdx.x, t = threadIdx.x, threads = blockDim.x;
+    cand += (size_t)b * K * n;
+    tok += (size_t)b * T;
+    pos += (size_t)b * T;
+    parent += (size_t)b * T;
+    node_of += (size_t)b * K * (n + 1);
+
+    for (int j = 0; j < n; ++j) {
+        for (int i = t; i < lay.slots; i += threads) {
+            keys[i] = 0;
+            low[i] = INT_MAX;
+        }
+        __syncthreads();
+        for (int k = t; k < K; k += threads) {
+            const int with = j == 0 ? 0 : first[k * n + j - 1], c = cand[k * n + j];
+            int at = -1;
+            if (with >= 0 && c >= 0) {
+                const unsigned long long key = ((unsigned long long)(with + 1) << 32) | (uint32_t)c;
+                at = (int)((key * 0x9e3779b97f4a7c15ull) >> 40) & (lay.slots - 1);
+                for (;;) {                      // at most half of the slots are taken
+                    const unsigned long long was = atomicCAS(&keys[at], 0ull, key);
+                    if (was == 0 || was == key) break;
+                    at = (at + 1) & (lay.slots - 1);
+                }
+                atomicMin(&low[at], k);
+            }
+            number[k * n + j] = at;
+        }
+        __syncthreads();
+        for (int k = t; k < K; k += threads) {
+            const int at = number[k * n + j];
+            first[k * n + j] = at < 0 ? -1 : low[at];
+        }
+        __syncthreads();
+    }
+    // every thread numbers a run of consecutive entries
+    const int run = (K * n + threads - 1) / threads, begin = min(t * run, K * n), end = min(begin + run, K * n);
+    int fresh = 0, total;
+    for (int i = begin; i < end; ++i) fresh += first[i] == i / n;
+    int next = 1 + block_inclusive_sum(fresh, part, total) - fresh;
+    for (int i = begin; i < end; ++i)
+        if (first[i] == i / n) number[i] = next++;
+    const int nodes = min(1 + total, T);
+    const int length = seq_len[b];
+    __syncthreads();
+    for (int i = t; i < K * n; i += threads) {
+        const int k = i / n, j = i - k * n;
+        const int node = first[i] < 0 ? -1 : number[first[i] * n + j];
+        node_of[k * (n + 1) + j + 1] = node < T ? node : -1;
+        if (j == 0) node_of[k * (n + 1)] = 0;
+        if (first[i] == k && node < T) {
+            const int above = j == 0 ? 0 : number[first[i - 1] * n + j - 1];
+            tok[node] = cand[i];
+            parent[node] = above;
+            pos[node] = length + j + 1;
+            up[node] = above;
+        }
+    }
+    for (int i = t; i < T; i += threads) {
+        if (i != 0 && i < nodes) continue;
+        tok[i] = i == 0 ? last_tok[b] : 0;
+        parent[i] = -1;
+        pos[i] = length;
+        up[i] = -1;
+    }
+    if (t == 0) n_nodes[b] = nodes;
+    __syncthreads();
+    const int words = (T + 31) / 32;
+    mask += (size_t)b * T * words;
+    for (int i = t; i < T * words; i += threads) {
+        const int node = i / words, w = i - node * words;
+        uint32_t bits = 0;
+        if (node < nodes)
+            for (int at = node; at >= 0; at = up[at])
+                if (at >> 5 == w) bits |= 1u << (at & 31);
+        mask[i] = bits;
+    }
+}
+
+// ---- block tables and slots ----------------------------------------------------------------------------------------
+// The prefix sum that deals the free pages needs all sequences, so one CTA grows the tables; it writes the slots too while
+// they are few, otherwise a second kernel does with the whole GPU.
+constexpr int kTableThreads = 1024;
+constexpr int kSlotThreads = 256;
+
+struct TableArgs {
+    const int32_t *seq_len, *n_new;          // n_new null: max_new everywhere
+    int B, page, max_new;
+    int32_t *table;                          // rows `stride` apart
+    long long stride;
+    int max_pages;
+    const int32_t *n_pages, *free_pages, *free_count;
+    int n_free;                              // entries of free_pages
+    int64_t *slots;                          // [B, max_new]
+    int32_t *n_pages_out, *free_count_out, *err;
+};
+
+__device__ __forceinline__ int in_range(int x, int lo, int hi, int32_t *err) {
+    if (x < lo || x > hi) report_error(err, SPEC_ERR_INDEX_RANGE);
+    return min(max(x, lo), hi);
+}
+
+// The slot of new token j of a sequence that has `held` pages.
+__device__ __forceinline__ int64_t slot_of(const TableArgs &a, int b, int j) {
+    const int length = max(a.seq_len[b], 0), fresh = a.n_new == nullptr ? a.max_new : min(a.n_new[b], a.max_new);
+    const long long at = (long long)length + j;
+    const int page = (int)(at / a.page);
+    if (j >= fresh || page >= a.n_pages_out[b]) return -1;
+    const int id = a.table[b * a.stride + page];
+    if (id < 0) {
+        report_error(a.err, SPEC_ERR_INDEX_RANGE);
+        return -1;
+    }
+    return (int64_t)id * a.page + (at - (long long)page * a.page);
+}
+
+__global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const TableArgs a, int with_slots) {
+    __shared__ int part[33];
+    __shared__ int held_s[kTableThreads], grow_s[kTableThreads], first_s[kTableThreads];
+    griddep_launch();
+    griddep_wait();
+    const int t = threadIdx.x, lane = t & 31;
+    const int avail = in_range(*a.free_count, 0, a.n_free, a.err);
+    long long asked = 0;                     // pages that the sequences before this block of them ask for
+    int taken = 0;                           // ... and get
+    for (int b0 = 0; b0 < a.B; b0 += kTableThreads) {
+        const int b = b0 + t, count = min(a.B - b0, kTableThreads);
+        int held = 0, need = 0;
+        if (b < a.B) {
+            const int length = in_range(a.seq_len[b], 0, INT_MAX, a.err);
+            const int fresh = a.n_new == nullptr ? a.max_new : in_range(a.n_new[b], 0, a.max_new, a.err);
+            held = in_range(a.n_pages[b], 0, a.max_pages, a.err);
+            const long long want = ((long long)length + fresh + a.page - 1) / a.page;
+            if (want > a.max_pages) report_error(a.err, SPEC_ERR_PAGES);
+            else need = max((int)want - held, 0);
+        }
+        int total;                           // at most B max_pages, which the host keeps within 32 bits
+        const int before = block_inclusive_sum(need, part, total) - need;
+        const bool fits = asked + before + need <= avail;
+        if (b < a.B) {
+            if (!fits && need > 0) report_error(a.err, SPEC_ERR_PAGES);
+            held_s[t] = held;
+            grow_s[t] = fits ? need : 0;
+            first_s[t] = (int)(avail - 1 - asked - before);    // only read where it fits
+            a.n_pages_out[b] = held + grow_s[t];
+        }
+        // The sums rise with the sequence: behind one that does not fit, only sequences that ask for nothing are served.
+        int dealt;
+        block_inclusive_sum(b < a.B ? grow_s[t] : 0, part, dealt);
+        __syncthreads();
+        for (int i = t >> 5; i < count; i += kTableThreads / 32)
+            for (int p = lane; p < grow_s[i]; p += 32)
+                a.table[(b0 + i) * a.stride + held_s[i] + p] = a.free_pages[first_s[i] - p];
+        asked += total;
+        taken += dealt;
+        __syncthreads();
+    }
+    if (t == 0) *a.free_count_out = avail - taken;
+    if (with_slots)
+        for (int i = t; i < a.B * a.max_new; i += kTableThreads) a.slots[i] = slot_of(a, i / a.max_new, i % a.max_new);
+}
+
+__global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(const TableArgs a) {
+    griddep_launch();
+    griddep_wait();
+    for (long long i = (long long)blockIdx.x * kSlotThreads + threadIdx.x; i < (long long)a.B * a.max_new;
+         i += (long long)gridDim.x * kSlotThreads)
+        a.slots[i] = slot_of(a, (int)(i / a.max_new), (int)(i % a.max_new));
+}
+
+// ---- the greedy walk -----------------------------------------------------------------------------------------------
+// A cluster of CTAs per sequence, each with a part of the vocabulary.  Per step: every CTA finds the maximum of its part of the
+// current node's row, the CTAs exchange theirs through distributed shared memory, and all of them look up the child
+// that carries the winner.  Only the rows on the path are read.  The constraints apply to what is read: the tokens of a
+// CTA's part that penalties or biases touch are counted in shared memory once and marked in a bitmap, so that a vector
+// of logits without a marked token costs what it costs without constraints.
+constexpr int kWalkThreads = 512;
+constexpr int kWalkWarps = kWalkThreads / 32;
+constexpr int kWalkMaxCluster = 8;
+constexpr int kNoToken = INT_MAX;
+constexpr uint32_t kSeen = 1u << 31;         // of a token's count: it is in the history (the rest: times it was generated)
+
+struct WalkArgs {
+    spec_tree_verify_t v;
+    int part;                                // vocabulary entries of a CTA, a multiple of 32
+    int pass;                                // ... that its tables in shared memory cover at a time, a multiple of 32
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void store_peer(const void *p, uint32_t rank, float x, int y) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(__float_as_uint(x)), "r"(y) : "memory");
+}
+
+template <int kDtype> struct Logit;
+template <> struct Logit<SPEC_BF16> {
+    static constexpr int kBytes = 2;
+    static __device__ __forceinline__ float get(const uint4 &v, int i) {
+        const uint32_t w = (&v.x)[i >> 1];
+        return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    }
+};
+template <> struct Logit<SPEC_F16> {
+    static constexpr int kBytes = 2;
+    static __device__ __forceinline__ float get(const uint4 &v, int i) {
+        const uint32_t w = (&v.x)[i >> 1];
+        return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w >> 16 : w & 0xffffu)));
+    }
+};
+template <> struct Logit<SPEC_F32> {
+    static constexpr int kBytes = 4;
+    static __device__ __forceinline__ float get(const uint4 &v, int i) { return __uint_as_float((&v.x)[i]); }
+};
+
+struct Best {
+    float value;
+    int tok;
+    __device__ __forceinline__ void offer(float x, int t) {
+        x = x != x ? -INFINITY : x;          // a NaN never wins
+        if (x > value || (x == value && t < tok)) {
+            value = x;
+            tok = t;
+        }
+    }
+};
+
+// Tables of one pass over a part of the vocabulary.
+struct WalkTables {
+    uint32_t *count;      // [pass] kSeen and the times generated
+    uint32_t *bias;       // [pass] entry of the bias list + 1, 0: none
+    uint32_t *marked;     // [pass / 32]
+};
+
+__device__ __forceinline__ void walk_count(const WalkTables &w, int t, bool generated) {
+    atomicOr(&w.marked[t >> 5], 1u << (t & 31));
+    atomicOr(&w.count[t], kSeen);
+    if (generated) atomicAdd(&w.count[t], 1u);
+}
+
+__device__ __forceinline__ float walk_adjust(const WalkArgs &a, const WalkTables &w, int b, int t, float x, float rep,
+                                             float freq, float pres) {
+    // Each step rounds once, in the order of the definition: no contraction into fused multiply-adds.
+    if (a.v.hist_tok != nullptr) {
+        const uint32_t c = w.count[t];
+        if (c & kSeen) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
+        const uint32_t times = c & ~kSeen;
+        if (times) x = __fsub_rn(__fsub_rn(x, __fmul_rn(freq, (float)times)), pres);
+    }
+    if (a.v.bias_tok != nullptr && w.bias[t])
+        x = __fadd_rn(x, a.v.bias_val[(size_t)b * a.v.max_bias + w.bias[t] - 1]);
+    return x;
+}
+
+template <int kDtype>
+__global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(const WalkArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ Best warp_best[kWalkWarps];
+    __shared__ __align__(8) Best peer_best[2][kWalkMaxCluster];
+    __shared__ int went[SPEC_MAX_TREE_DEPTH];     // tokens taken so far
+    __shared__ int child;
+    griddep_launch();
+    griddep_wait();
+    constexpr int kPer = 16 / Logit<kDtype>::kBytes;
+    const int t = threadIdx.x, lane = t & 31;
+    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    const int b = blockIdx.x / ranks;
+    const spec_tree_verify_t &v = a.v;
+    const int V = v.V, lo = min((int)rank * a.part, V), hi = min(lo + a.part, V);
+    const bool listed = v.hist_tok != nullptr || v.bias_tok != nullptr;
+    WalkTables w;
+    w.count = (uint32_t *)smem;
+    w.bias = w.count + (v.hist_tok != nullptr ? a.pass : 0);
+    w.marked = w.bias + (v.bias_tok != nullptr ? a.pass : 0);
+    const int nodes = min(v.n_nodes[b], v.T);
+    const float rep = v.repetition != nullptr ? v.repetition[b] : 1.f;
+    const float freq = v.frequency != nullptr ? v.frequency[b] : 0.f;
+    const float pres = v.presence != nullptr ? v.presence[b] : 0.f;
+    const int32_t *tok = v.tok + (size_t)b * v.T, *parent = v.parent + (size_t)b * v.T;
+    const int words = (V + 31) / 32;
+
+    int cur = 0, accepted = 0, token = -1;
+    if (nodes > 0) {
+        for (int step = 0;; ++step) {
+            Best best = {-INFINITY, kNoToken};
+            const char *row = (const char *)v.logits + ((long long)b * v.logits_stride[0] + (long long)cur * v.logits_stride[1]) *
+                                                           Logit<kDtype>::kBytes;
+            const uint32_t *allow = v.allow == nullptr ? nullptr : v.allow + ((size_t)b * v.T + cur) * words;
+            const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);   // elements behind a vector's start
+            const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
+            for (int p0 = lo; p0 < hi; p0 += a.pass) {
+                const int p1 = min(p0 + a.pass, hi);
+                if (listed && (step == 0 || a.pass < a.part)) {
+                    const int all = (v.hist_tok != nullptr ? a.pass : 0) + (v.bias_tok != nullptr ? a.pass : 0) + a.pass / 32;
+                    __syncthreads();
+                    for (int i = t; i < all; i += kWalkThreads) ((uint32_t *)smem)[i] = 0;
+                    __syncthreads();
+                    if (v.hist_tok != nullptr) {
+                        const int size = min(v.hist_len[b], v.max_hist), prompt = v.prompt_len == nullptr ? 0 : v.prompt_len[b];
+                        const int32_t *hist = v.hist_tok + (size_t)b * v.max_hist;
+                        for (int i = t; i < size + step; i += kWalkThreads) {
+                            const int h = i < size ? hist[i] : went[i - size];
+                            if (h >= p0 && h < p1) walk_count(w, h - p0, i >= prompt || i >= size);
+                        }
+                    }
+                    if (v.bias_tok != nullptr) {
+                        const int size = v.bias_len == nullptr ? v.max_bias : min(v.bias_len[b], v.max_bias);
+                        for (int i = t; i < size; i += kWalkThreads) {
+                            const int h = v.bias_tok[(size_t)b * v.max_bias + i];
+                            if (h < p0 || h >= p1) continue;
+                            atomicOr(&w.marked[(h - p0) >> 5], 1u << ((h - p0) & 31));
+                            atomicMax(&w.bias[h - p0], (uint32_t)i + 1);     // the list's last entry counts
+                        }
+                    }
+                    __syncthreads();
+                }
+                // vectors that hold elements of [p0, p1); the row's first and last one may reach beyond it into memory that belongs
+                // to other rows or to nobody, so those are read element by element
+                const int v0 = (p0 + skew) / kPer, v1 = (p1 + skew + kPer - 1) / kPer;
+                for (int i = v0 + t; i < v1; i += kWalkThreads) {
+                    const int e0 = i * kPer - skew;
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (e0 >= 0 && e0 + kPer <= V) {
+                        x = __ldg(vec + i);
+                    } else {
+                        for (int e = max(e0, 0); e < min(e0 + kPer, V); ++e) {
+                            if (Logit<kDtype>::kBytes == 2) ((uint16_t *)&x)[e - e0] = ((const uint16_t *)row)[e];
+                            else (&x.x)[e - e0] = ((const uint32_t *)row)[e];
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) {
+                        const int at = e0 + e;
+                        if (at < p0 || at >= p1) continue;
+                        if (allow != nullptr && !(allow[at >> 5] >> (at & 31) & 1)) continue;
+                        float y = Logit<kDtype>::get(x, e);
+                        if (listed && (w.marked[(at - p0) >> 5] >> ((at - p0) & 31) & 1))
+                            y = walk_adjust(a, w, b, at - p0, y, rep, freq, pres);
+                        best.offer(y, at);
+                    }
+                }
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) {
+                const float ov = __shfl_xor_sync(0xffffffffu, best.value, off);
+                const int ot = __shfl_xor_sync(0xffffffffu, best.tok, off);
+                best.offer(ov, ot);
+            }
+            if (lane == 0) warp_best[t >> 5] = best;
+            if (t == 0) child = INT_MAX;
+            __syncthreads();
+            if (t < 32) {
+                best = t < kWalkWarps ? warp_best[t] : Best{-INFINITY, kNoToken};
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) {
+                    const float ov = __shfl_xor_sync(0xffffffffu, best.value, off);
+                    const int ot = __shfl_xor_sync(0xffffffffu, best.tok, off);
+                    best.offer(ov, ot);
+                }
+                if (t < ranks) store_peer(&peer_best[step & 1][rank], t, best.value, best.tok);
+            }
+            cluster_sync();
+            best = {-INFINITY, kNoToken};
+            for (int r = 0; r < (int)ranks; ++r) best.offer(peer_best[step & 1][r].value, peer_best[step & 1][r].tok);
+            token = best.tok == kNoToken ? -1 : best.tok;
+            if (rank == 0 && t == 0) v.path[(size_t)b * (v.n + 1) + step] = cur;
+            if (step == v.n || token < 0) break;
+            for (int i = 1 + t; i < nodes; i += kWalkThreads)
+                if (parent[i] == cur && tok[i] == token) atomicMin(&child, i);
+            if (t == 0) went[step] = token;
+            if (v.hist_tok != nullptr && a.pass >= a.part && t == 0 && token >= lo && token < hi)
+                walk_count(w, token - lo, true);
+            __syncthreads();
+            if (child == INT_MAX) break;
+            cur = child;
+            ++accepted;
+            __syncthreads();
+        }
+    }
+    cluster_sync();                          // no CTA leaves while another may still write to its shared memory
+    if (rank == 0) {
+        if (t == 0) {
+            v.accept_len[b] = accepted;
+            v.last_node[b] = nodes > 0 ? cur : -1;
+            v.next_tok[b] = token;
+        }
+        for (int j = (nodes > 0 ? accepted + 1 : 0) + t; j <= v.n; j += kWalkThreads) v.path[(size_t)b * (v.n + 1) + j] = -1;
+    }
+}
+
+// ---- accepted keys and values --------------------------------------------------------------------------------------
+constexpr int kCommitThreads = 256;
+
+__global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv_commit_t c) {
+    griddep_launch();
+    griddep_wait();
+    const int b = blockIdx.y, n1 = c.n + 1;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && c.new_len != nullptr)
+        c.new_len[b] = c.seq_len[b] + min(max(c.accept_len[b], -1), c.n) + 1;
+    const int per_head = c.D / 8, per_row = c.H * per_head;
+    const long long i = (long long)blockIdx.x * kCommitThreads + threadIdx.x;
+    if (i >= 2ll * c.L * per_row) return;
+    const int vec = (int)(i % per_row), layer = (int)(i / per_row) % c.L;
+    const bool is_v = i / per_row >= c.L;
+    const int head = vec / per_head, d = (vec - head * per_head) * 8;
+    const int64_t *ss = is_v ? c.v_stride : c.k_stride, *ds = is_v ? c.vc_stride : c.kc_stride;
+    const uint16_t *src = (const uint16_t *)(is_v ? c.v : c.k) + layer * ss[0] + b * ss[1] + head * ss[3] + d;
+    uint16_t *dst = (uint16_t *)(is_v ? c.v_cache : c.k_cache) + layer * ds[0] + head * ds[3] + d;
+    const int rows = min(c.accept_len[b], c.n) + 1;
+    for (int j = 0; j < rows; ++j) {
+        const int node = c.path[(size_t)b * n1 + j];
+        const long long slot = c.slots[(size_t)b * n1 + j];
+        if (node < 0 || node >= c.T || slot < 0 || slot >= (long long)c.n_pages * c.page_size) {
+            report_error(c.err_word, SPEC_ERR_INDEX_RANGE);
+            continue;
+        }
+        const uint4 x = *(const uint4 *)(src + node * ss[2]);
+        const long long page = slot / c.page_size;
+        *(uint4 *)(dst + page * ds[1] + (slot - page * c.page_size) * ds[2]) = x;
+    }
+}
+
+template <int kDtype>
+int launch_walk(const WalkArgs &a, int ctas, size_t smem, cudaStream_t st) {
+    SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_walk_kernel<kDtype>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    SPEC_CUDA_TRY(launch_pdl_cluster(tree_walk_kernel<kDtype>, dim3(ctas * a.v.B), dim3(kWalkThreads), smem, ctas, st, a));
+    return SPEC_OK;
+}
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+}  // namespace spec
+
+using namespace spec;
+
+extern "C" {
+
+int spec_tree_plan(const int32_t *cand_tok, const int32_t *last_tok, const int32_t *seq_len, int B, int K, int n, int T,
+                   int32_t *tok, int32_t *pos, int32_t *parent, uint32_t *mask, int32_t *node_of, int32_t *n_nodes,
+                   void *cuda_stream) {
+    if (!cand_tok || !last_tok || !seq_len || !tok || !pos || !parent || !mask || !node_of || !n_nodes)
+        return SPEC_ERR_INVALID_ARG;
+    if (B <= 0 || K <= 0 || n <= 0 || T <= 0) return SPEC_ERR_INVALID_ARG;
+    if (n > SPEC_MAX_TREE_DEPTH || T > SPEC_MAX_TREE_NODES || K > SPEC_MAX_LEAVES || (long long)K * n > SPEC_MAX_TREE_ENTRIES)
+        return SPEC_ERR_SHAPE;
+    const PlanSmem lay = plan_smem(K, n, T);
+    if (lay.total > 40 * 1024)
+        SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lay.total));
+    int threads = K * n > T ? K * n : T;
+    threads = threads >= kPlanMaxThreads ? kPlanMaxThreads : (threads + 31) / 32 * 32;
+    SPEC_CUDA_TRY(launch_pdl(tree_plan_kernel, dim3(B), dim3(threads), (size_t)lay.total, (cudaStream_t)cuda_stream, cand_tok,
+                             last_tok, seq_len, K, n, T, tok, pos, parent, mask, node_of, n_nodes));
+    return SPEC_OK;
+}
+
+int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int page_size, int max_new, int32_t *block_table,
+                     int64_t table_stride, int max_pages, const int32_t *n_pages, const int32_t *free_pages,
+                     const int32_t *free_count, int n_free, int64_t *slots, int32_t *n_pages_out, int32_t *free_count_out,
+                     int32_t *err_word, void *cuda_stream) {
+    if (!seq_len || !block_table || !n_pages || !free_pages || !free_count || !slots || !n_pages_out || !free_count_out)
+        return SPEC_ERR_INVALID_ARG;
+    if (B <= 0 || page_size <= 0 || max_new <= 0 || max_pages <= 0 || n_free <= 0) return SPEC_ERR_INVALID_ARG;
+    if (table_stride < max_pages || (long long)B * max_new > INT_MAX || (long long)B * max_pages > INT_MAX) return SPEC_ERR_SHAPE;
+    const TableArgs a = {seq_len, n_new, B, page_size, max_new, block_table, table_stride, max_pages, n_pages, free_pages,
+                         free_count, n_free, slots, n_pages_out, free_count_out, err_word};
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const int all = B * max_new;
+    const bool one = all <= 4 * kTableThreads;
+    SPEC_CUDA_TRY(launch_pdl(page_tables_kernel, dim3(1), dim3(kTableThreads), 0, st, a, one ? 1 : 0));
+    if (!one) {
+        const int blocks = (all + kSlotThreads - 1) / kSlotThreads, most = 8 * num_sms();
+        SPEC_CUDA_TRY(launch_pdl(page_slots_kernel, dim3(blocks < most ? blocks : most), dim3(kSlotThreads), 0, st, a));
+    }
+    return SPEC_OK;
+}
+
+int spec_verify_tree(const spec_tree_verify_t *v, void *cuda_stream) {
+    if (!v || !v->tok || !v->parent || !v->n_nodes || !v->logits || !v->accept_len || !v->last_node || !v->next_tok || !v->path)
+        return SPEC_ERR_INVALID_ARG;
+    if (v->B <= 0 || v->T <= 0 || v->V <= 0 || v->n < 0) return SPEC_ERR_INVALID_ARG;
+    if (v->logits_dtype != SPEC_BF16 && v->logits_dtype != SPEC_F16 && v->logits_dtype != SPEC_F32) return SPEC_ERR_INVALID_ARG;
+    if ((uintptr_t)v->logits % (v->logits_dtype == SPEC_F32 ? 4 : 2) != 0) return SPEC_ERR_INVALID_ARG;
+    if (v->logits_stride[0] < 0 || v->logits_stride[1] < 0) return SPEC_ERR_INVALID_ARG;
+    if (v->hist_tok && (!v->hist_len || v->max_hist <= 0)) return SPEC_ERR_INVALID_ARG;
+    if (!v->hist_tok && (v->repetition || v->frequency || v->presence || v->prompt_len)) return SPEC_ERR_INVALID_ARG;
+    if (v->bias_tok && (!v->bias_val || v->max_bias <= 0)) return SPEC_ERR_INVALID_ARG;
+    if (v->n > SPEC_MAX_TREE_DEPTH || v->T > SPEC_MAX_TREE_NODES || v->B > (1 << 20) || v->V > (1 << 30) ||
+        v->max_hist > (1 << 30) || v->max_bias > (1 << 30))
+        return SPEC_ERR_SHAPE;
+    WalkArgs a;
+    a.v = *v;
+    int ctas = 1;
+    while (ctas < kWalkMaxCluster && (long long)ctas * 2048 < v->V) ctas *= 2;
+    a.part = ((v->V + ctas - 1) / ctas + 31) / 32 * 32;
+    const int arrays = (v->hist_tok ? 1 : 0) + (v->bias_tok ? 1 : 0);
+    // as much of the part as 160 KB of tables cover at a time
+    a.pass = a.part;
+    const int cover = 160 * 1024 / (4 * arrays + 1) / 32 * 32;
+    if (arrays && a.pass > cover) a.pass = cover;
+    const size_t smem = arrays ? ((size_t)a.pass * arrays + a.pass / 32) * 4 : 0;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (v->logits_dtype == SPEC_BF16) return launch_walk<SPEC_BF16>(a, ctas, smem, st);
+    if (v->logits_dtype == SPEC_F16) return launch_walk<SPEC_F16>(a, ctas, smem, st);
+    return launch_walk<SPEC_F32>(a, ctas, smem, st);
+}
+
+int spec_kv_commit(const spec_kv_commit_t *c, void *cuda_stream) {
+    if (!c || !c->k || !c->v || !c->k_cache || !c->v_cache || !c->path || !c->accept_len || !c->slots) return SPEC_ERR_INVALID_ARG;
+    if (c->new_len && !c->seq_len) return SPEC_ERR_INVALID_ARG;
+    if (c->L <= 0 || c->B <= 0 || c->T <= 0 || c->n < 0 || c->H <= 0 || c->D <= 0 || c->page_size <= 0 || c->n_pages <= 0)
+        return SPEC_ERR_INVALID_ARG;
+    if (c->D % 8 != 0 || c->B > 65535 || (long long)c->L * c->H * c->D > INT_MAX / 4) return SPEC_ERR_SHAPE;
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_cache) || !aligned16(c->v_cache)) return SPEC_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i) {
+        if (c->k_stride[i] % 8 || c->v_stride[i] % 8 || c->kc_stride[i] % 8 || c->vc_stride[i] % 8) return SPEC_ERR_SHAPE;
+        if (c->k_stride[i] < 0 || c->v_stride[i] < 0 || c->kc_stride[i] < 0 || c->vc_stride[i] < 0) return SPEC_ERR_INVALID_ARG;
+    }
+    const long long vecs = 2ll * c->L * c->H * (c->D / 8);
+    SPEC_CUDA_TRY(launch_pdl(kv_commit_kernel, dim3((unsigned)((vecs + kCommitThreads - 1) / kCommitThreads), c->B),
+                             dim3(kCommitThreads), 0, (cudaStream_t)cuda_stream, *c));
+    return SPEC_OK;
+}
+
+}  // extern "C"
