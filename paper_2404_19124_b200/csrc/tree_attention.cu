@@ -1,99 +1,863 @@
-// Attention of a tree of drafted tokens over a paged cache and the tree itself.
+// Attention of a tree of drafted tokens over a paged cache and the tree itself: softmax(scale Q K^T + mask) V with the scores
+// and the sums on the tensor cores (tcgen05), fp32 in TMEM.
+//
+// Work.  A unit is a sequence, a key head and up to 256 of the query rows that share it (row = node * group + head within the
+// group); its keys, the cache's and then the tree's, are cut into tiles of 128.  All tiles of all units in a row are dealt to
+// the CTAs, one per SM, in equal runs, so that ragged batches and few long sequences fill the GPU alike.  A unit that a CTA
+// has to itself is written straight to `out`; of the others every CTA leaves its rows, normalised, with their log-sum-exp in
+// the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
+//
+// Roles of a CTA (13 warps):
+//   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
+//                   TMEM in place of the scores, results
+//   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 128], O += P V, P read from TMEM
+//   warps 9-12      gather rows of Q, K and V with 16-byte asynchronous copies (pages of any size, any strides; rows that do
+//                   not exist read as zeros) into 128-byte-swizzled tiles
+// Two streams keep the tensor cores busy while a softmax runs.  Units of more than 128 rows have a stream per 128 rows, both on the
+// same tile of keys; smaller ones give their tiles to the streams in turn, and the two results are joined at the end.
 #include <limits.h>
 #include <math.h>
 
 #include <cuda_fp16.h>
 
 #include "spec_common.cuh"
+#include "tc_gemm.cuh"
 
 namespace spec {
 
 namespace {
 
-constexpr int kSimpleThreads = 128;
+using tc::ex2_approx;
+using tc::mbar_arrive;
+using tc::mbar_init;
+using tc::mbar_try_wait;
+using tc::smem_u32;
+using tc::tc_fence_after;
+using tc::tc_fence_before;
+using tc::tmem_ld32;
+using tc::umma_commit;
 
-template <int kDtype> __device__ __forceinline__ float to_float(uint16_t x) {
-    return kDtype == SPEC_BF16 ? bf16_bits_to_float(x) : __half2float(__ushort_as_half(x));
-}
-template <int kDtype> __device__ __forceinline__ uint16_t from_float(float x) {
-    return kDtype == SPEC_BF16 ? (uint16_t)float_to_bf16_bits(x) : __half_as_ushort(__float2half_rn(x));
-}
+constexpr int kTileKeys = 128;
+constexpr int kTileRows = 128;
+constexpr int kHalfBytes = kTileKeys * 128;     // 64 columns of a tile of 128 rows
+constexpr int kSoftmaxThreads = 256;
+constexpr int kLoadThreads = 128;
+constexpr int kFirstLoader = kSoftmaxThreads + 32;
+constexpr int kThreads = kFirstLoader + kLoadThreads;
+constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns each
+constexpr int kUnitFlags = 8;
+constexpr float kRescaleAbove = 8.f;            // see softmax_tile
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
-template <bool kMax>
-__device__ float block_reduce(float x, float *part) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const float y = __shfl_xor_sync(0xffffffffu, x, off);
-        x = kMax ? fmaxf(x, y) : x + y;
+// Columns come in halves of 64: D <= 64 takes one, and twice the slots.
+template <int kHalves>
+struct Ring {
+    static constexpr int kBytes = kHalves * kHalfBytes;
+    static constexpr int kK = kHalves == 2 ? 3 : 6, kV = kHalves == 2 ? 2 : 5, kQ = 2;
+};
+constexpr int kMaxK = 6, kMaxV = 5;
+
+struct Shared {
+    uint64_t q_full[2], q_empty[2], k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
+    uint64_t s_full[2], p_full[2], pv_done[2], meet, drained;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see load_v)
+    int start_b;
+    long long start_off, pos, end;
+    float stat[2][kTileRows][2];                // running maximum and sum of the two streams
+};
+template <int kHalves>
+constexpr int smem_bytes() {
+    return (Ring<kHalves>::kK + Ring<kHalves>::kV + Ring<kHalves>::kQ) * Ring<kHalves>::kBytes + (int)sizeof(Shared);
+}
+static_assert(smem_bytes<2>() <= 232448 && smem_bytes<1>() <= 232448, "shared memory of an SM");
+
+struct AttnArgs {
+    spec_tree_attention_t a;
+    int group;                // query heads per key head
+    float scale_log2;         // |scale| log2(e)
+    uint32_t desc_qk, desc_pv;
+    float *part_out;          // [2 * CTAs][part_rows][D]
+    float *part_lse;          // [2 * CTAs][part_rows]
+    int part_rows;
+};
+
+__device__ __noinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
+    for (uint32_t it = 0; it < tc::kSpinMax; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (it > tc::kSpinFast) {
+            if (sh->abort_flag) return false;
+            __nanosleep(64);
+        }
     }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = part[0];
-    for (int i = 1; i < kSimpleThreads / 32; ++i) x = kMax ? fmaxf(x, part[i]) : x + part[i];
+    sh->abort_flag = 1;
+    report_error(err, SPEC_ERR_TIMEOUT);
+    return false;
+}
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
+    return mbar_try_wait(bar, parity) || poll(bar, parity, sh, err);
+}
+// The whole warp waits, leaves converged and with one verdict.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
+    return __all_sync(0xffffffffu, wait(bar, parity, sh, err));
+}
+
+// ---- work ------------------------------------------------------------------------------------------------------------
+struct Seq {
+    int len, nodes, units, tiles;      // tiles: per unit
+};
+
+__device__ __forceinline__ Seq seq_of(const AttnArgs &g, int b, bool report) {
+    const spec_tree_attention_t &a = g.a;
+    const int cap = (int)min((long long)a.max_pages * a.page_size, (long long)INT_MAX - 4096);
+    const int len = a.seq_len[b], nodes = a.n_nodes != nullptr ? a.n_nodes[b] : a.T;
+    Seq s;
+    s.len = min(max(len, 0), cap);
+    s.nodes = min(max(nodes, 0), a.T);
+    if (report && (s.len != len || s.nodes != nodes)) report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
+    s.units = a.Hkv * ((s.nodes * g.group + 2 * kTileRows - 1) / (2 * kTileRows));
+    s.tiles = (s.len + s.nodes + kTileKeys - 1) / kTileKeys;
+    return s;
+}
+
+__device__ __forceinline__ long long warp_inclusive_sum(long long x) {
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, off);
+        if ((threadIdx.x & 31) >= off) x += y;
+    }
     return x;
 }
 
-// One CTA per (query head, node, sequence): a thread per key for the scores, a thread per column for the sum of the values.
+// All tiles of the call; whole warp.
+__device__ long long all_tiles(const AttnArgs &g, bool report) {
+    long long sum = 0;
+    for (int b = threadIdx.x & 31; b < g.a.B; b += 32) {
+        const Seq s = seq_of(g, b, report);
+        sum += (long long)s.units * s.tiles;
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    return sum;
+}
+
+// The sequence that tile `pos` belongs to and the tile's place in it; whole warp.  B if there is none.
+__device__ int find_tile(const AttnArgs &g, long long pos, long long &off) {
+    long long before = 0;
+    for (int b0 = 0; b0 < g.a.B; b0 += 32) {
+        const int b = b0 + (threadIdx.x & 31);
+        long long mine = 0;
+        if (b < g.a.B) {
+            const Seq s = seq_of(g, b, false);
+            mine = (long long)s.units * s.tiles;
+        }
+        const long long upto = before + warp_inclusive_sum(mine);
+        const unsigned hit = __ballot_sync(0xffffffffu, upto > pos);
+        if (hit) {
+            const int lane = __ffs(hit) - 1;
+            off = pos - __shfl_sync(0xffffffffu, upto - mine, lane);
+            return b0 + lane;
+        }
+        before = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    off = 0;
+    return g.a.B;
+}
+
+__device__ __forceinline__ long long cta_start(long long tiles, int cta, int ctas) { return tiles * cta / ctas; }
+
+// A unit's tiles [t0, t1) that this CTA has.
+struct Unit {
+    int b, head, row0, rows;           // rows row0 .. row0 + rows - 1 of the head's nodes * group
+    int len, nodes, tiles, t0, t1;
+    int index;                         // counts the CTA's units
+    __device__ bool two_tiles() const { return rows > kTileRows; }
+    __device__ bool whole() const { return t0 == 0 && t1 == tiles; }
+};
+
+struct Walk {
+    Seq s;
+    int b, unit, tile, index;
+    long long pos, end;
+    __device__ Walk(const AttnArgs &g, const Shared *sh) {
+        b = sh->start_b;
+        pos = sh->pos;
+        end = sh->end;
+        index = 0;
+        unit = tile = 0;
+        s = {0, 0, 0, 0};
+        if (b < g.a.B) {
+            s = seq_of(g, b, false);
+            unit = (int)(sh->start_off / s.tiles);
+            tile = (int)(sh->start_off - (long long)unit * s.tiles);
+        }
+    }
+    __device__ bool next(const AttnArgs &g, Unit &u) {
+        while (pos < end && b < g.a.B) {
+            if (unit >= s.units) {
+                unit = tile = 0;
+                if (++b < g.a.B) s = seq_of(g, b, false);
+                continue;
+            }
+            const int blocks = s.units / g.a.Hkv, head = unit / blocks;
+            u.b = b;
+            u.head = head;
+            u.row0 = (unit - head * blocks) * 2 * kTileRows;
+            u.rows = min(s.nodes * g.group - u.row0, 2 * kTileRows);
+            u.len = s.len;
+            u.nodes = s.nodes;
+            u.tiles = s.tiles;
+            u.t0 = tile;
+            u.t1 = (int)min((long long)s.tiles, tile + (end - pos));
+            u.index = index++;
+            pos += u.t1 - u.t0;
+            tile = u.t1;
+            if (tile == s.tiles) {
+                ++unit;
+                tile = 0;
+            }
+            return true;
+        }
+        return false;
+    }
+};
+
+// ---- loads -----------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void arrive_when_copied(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// A tile is 128 rows of 8 (D <= 64) or 16 chunks of 16 bytes: chunk c of row r lies at half c / 8, row pitch 128, column
+// (c % 8) ^ (r % 8) of the row (the 128-byte swizzle of the MMA's descriptors).  A warp copies kRows rows at a time, in kPasses;
+// lane l knows where row own_row() comes from and hands that to the lanes that copy it.
+template <int kHalves>
+struct TileMap {
+    static constexpr int kChunks = 8 * kHalves, kRows = 32 / kChunks, kPasses = 32 / kRows, kStep = 4 * kRows;
+    int warp, lane, chunk, row;        // row: of pass 0
+    __device__ TileMap() {
+        const int t = threadIdx.x - kFirstLoader;
+        warp = t >> 5;
+        lane = t & 31;
+        chunk = lane % kChunks;
+        row = warp * kRows + lane / kChunks;
+    }
+    __device__ int own_row() const { return lane / kRows * kStep + warp * kRows + lane % kRows; }
+    // src: where own_row() starts, null: zeros.  cols: columns of a row in memory; the chunks up to a multiple of 16 are zeros.
+    __device__ void copy(uint32_t tile, const uint16_t *src, int cols) const {
+        const bool wanted = chunk * 8 < (cols + 15) / 16 * 16, there = chunk * 8 < cols;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const uint16_t *p = (const uint16_t *)__shfl_sync(0xffffffffu, (unsigned long long)src, i * kRows + lane / kChunks);
+            const int r = row + i * kStep;
+            const bool real = there && p != nullptr;
+            if (wanted) copy16(address(tile, r), real ? p + chunk * 8 : nullptr, real);
+        }
+    }
+    __device__ uint32_t address(uint32_t tile, int r) const {
+        return tile + (chunk >> 3) * kHalfBytes + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
+    }
+};
+
+// Where key `key` of a unit lies: page and token of the cache, or node of the tree.
+struct KeyPlace {
+    int page, token;                   // page -1: a node (token), -2: nothing
+};
+__device__ __forceinline__ KeyPlace key_place(const spec_tree_attention_t &a, const Unit &u, int key) {
+    KeyPlace p = {-2, 0};
+    if (key < u.len) {
+        const int page = key / a.page_size, id = a.block_table[u.b * a.table_stride + page];
+        if (id >= 0 && id < a.n_pages) p = {id, key - page * a.page_size};
+        else report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
+    } else if (key < u.len + u.nodes) {
+        p = {-1, key - u.len};
+    }
+    return p;
+}
+__device__ __forceinline__ const uint16_t *row_of(KeyPlace p, int b, int head, const void *cache, const int64_t *cs,
+                                                  const void *tree, const int64_t *ts) {
+    if (p.page >= 0) return (const uint16_t *)cache + p.page * cs[0] + p.token * cs[1] + head * cs[2];
+    if (p.page == -1) return (const uint16_t *)tree + b * ts[0] + p.token * ts[1] + head * ts[2];
+    return nullptr;
+}
+
+// Is one of the eight numbers not finite?  (bf16 has eight exponent bits, fp16 five.)
 template <int kDtype>
-__global__ void __launch_bounds__(kSimpleThreads) tree_attention_kernel(const spec_tree_attention_t a) {
-    __shared__ float q[128], p[kSimpleThreads], part[kSimpleThreads / 32];
-    __shared__ const uint16_t *val[kSimpleThreads];
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x, bool &bad) {
+    constexpr uint32_t kExp = kDtype == SPEC_BF16 ? 0x7f80u : 0x7c00u;
+    if ((x & kExp) == kExp) {
+        bad = true;
+        x &= 0xffff0000u;
+    }
+    if ((x >> 16 & kExp) == kExp) {
+        bad = true;
+        x &= 0x0000ffffu;
+    }
+    return x;
+}
+
+template <int kDtype, int kHalves>
+__device__ void load_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
+    using R = Ring<kHalves>;
+    const spec_tree_attention_t &a = g.a;
+    const TileMap<kHalves> map;
+    int qs = 0, ks = 0, vs = 0;                          // slots, and the parity of their `empty` that means free
+    uint32_t qp = 1, kp = 1, vp = 1;
+    Walk walk(g, sh);
+    Unit u;
+    while (walk.next(g, u)) {
+        for (int i = 0; i < (u.two_tiles() ? 2 : 1); ++i) {
+            if (!warp_wait(&sh->q_empty[qs], qp, sh, a.err_word)) return;
+            const int r = i * kTileRows + map.own_row(), node = (u.row0 + r) / g.group;
+            const uint16_t *src = nullptr;
+            if (r < u.rows)
+                src = (const uint16_t *)a.q + u.b * a.q_stride[0] + node * a.q_stride[1] +
+                      (u.head * g.group + u.row0 + r - node * g.group) * a.q_stride[2];
+            map.copy(q_tiles + qs * R::kBytes, src, a.D);
+            arrive_when_copied(&sh->q_full[qs]);
+            if (++qs == R::kQ) qs = 0, qp ^= 1;
+        }
+        // K of a tile goes ahead of V of the tile before
+        KeyPlace here = key_place(a, u, u.t0 * kTileKeys + map.own_row()), before = here;
+        for (int t = u.t0; t <= u.t1; ++t) {
+            KeyPlace ahead = here;
+            if (t < u.t1) {
+                if (t + 1 < u.t1) ahead = key_place(a, u, (t + 1) * kTileKeys + map.own_row());
+                if (!warp_wait(&sh->k_empty[ks], kp, sh, a.err_word)) return;
+                map.copy(k_tiles + ks * R::kBytes, row_of(here, u.b, u.head, a.k_cache, a.kc_stride, a.k, a.k_stride), a.D);
+                arrive_when_copied(&sh->k_full[ks]);
+                if (++ks == R::kK) ks = 0, kp ^= 1;
+            }
+            if (t > u.t0) {
+                if (!warp_wait(&sh->v_empty[vs], vp, sh, a.err_word)) return;
+                const uint32_t tile = v_tiles + vs * R::kBytes;
+                map.copy(tile, row_of(before, u.b, u.head, a.v_cache, a.vc_stride, a.v, a.v_stride), a.D);
+                const int key0 = (t - 1) * kTileKeys;
+                if (key0 + kTileKeys > u.len) {
+                    // Rows of the tree are not seen by every query, and 0 * inf would reach those that do not: what is not finite is
+                    // zero in the tile, and the unit's result takes it from memory (add_not_finite).
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    bool bad = false;
+                    if (map.chunk * 8 < a.D) {
+                        for (int i = 0; i < TileMap<kHalves>::kPasses; ++i) {
+                            const int r = map.row + i * TileMap<kHalves>::kStep;
+                            if (key0 + r < u.len || key0 + r >= u.len + u.nodes) continue;
+                            const uint32_t at = map.address(tile, r);
+                            uint32_t x[4];
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+                            bool found = false;
+                            for (int e = 0; e < 4; ++e) x[e] = finite_or_zero<kDtype>(x[e], found);
+                            if (found)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                             ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                            bad |= found;
+                        }
+                    }
+                    if (bad) sh->not_finite[u.index % kUnitFlags] = 1;
+                    fence_async_proxy();
+                    mbar_arrive(&sh->v_full[vs]);
+                } else {
+                    arrive_when_copied(&sh->v_full[vs]);
+                }
+                if (++vs == R::kV) vs = 0, vp ^= 1;
+            }
+            before = here;
+            here = ahead;
+        }
+    }
+}
+
+// ---- MMAs ------------------------------------------------------------------------------------------------------------
+// Descriptors: 128-byte swizzle.  Q and K are K-major (rows of 128 bytes, groups of 8 rows 1024 bytes apart).  V is MN-major: 64
+// columns of a key are contiguous, 8 keys make a 1024-byte group, the next 64 columns are kHalfBytes away.
+__device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
+    return tc::make_smem_desc(saddr) | (uint64_t)(kHalfBytes >> 4) << 16;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+
+template <int kHalves>
+__device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
+    using R = Ring<kHalves>;
+    int32_t *err = g.a.err_word;
+    const uint32_t tmem = sh->tmem_base;
+    const int k_steps = (g.a.D + 15) / 16;
+    int qs = 0, ks = 0, vs = 0;
+    uint32_t qp = 0, kp = 0, vp = 0, pp[2] = {0, 0};
+    Walk walk(g, sh);
+    Unit u;
+    while (walk.next(g, u)) {
+        const bool two = u.two_tiles();
+        const int steps = (u.t1 - u.t0) * (two ? 2 : 1);
+        // slots of the unit's query tiles
+        const int q0 = qs, q1 = two ? qs ^ 1 : qs;
+        const uint32_t qp0 = qp, qp1 = two && qs == 1 ? qp ^ 1 : qp;
+        if (!two) {
+            if (++qs == R::kQ) qs = 0, qp ^= 1;
+        } else {
+            qp ^= 1;
+        }
+        auto scores = [&](int j) -> bool {
+            const int s = j & 1, q = s ? q1 : q0;
+            if (j < 2 && !wait(&sh->q_full[q], s ? qp1 : qp0, sh, err)) return false;
+            if (!wait(&sh->k_full[ks], kp, sh, err)) return false;
+            fence_async_proxy();
+            const uint32_t qa = q_tiles + q * R::kBytes, ka = k_tiles + ks * R::kBytes;
+            for (int i = 0; i < k_steps; ++i) {
+                const uint32_t off = (i >> 2) * kHalfBytes + (i & 3) * 32;
+                mma_ss(tmem + s * 128, tc::make_smem_desc(qa + off), tc::make_smem_desc(ka + off), g.desc_qk, i > 0);
+            }
+            umma_commit(&sh->s_full[s]);
+            if (!two || s) {
+                umma_commit(&sh->k_empty[ks]);
+                if (++ks == R::kK) ks = 0, kp ^= 1;
+            }
+            if (j >= steps - (two ? 2 : 1)) umma_commit(&sh->q_empty[q]);
+            return true;
+        };
+        for (int j = 0; j < 2 && j < steps; ++j)
+            if (!scores(j)) return false;
+        for (int j = 0; j < steps; ++j) {
+            const int s = j & 1;
+            if (!wait(&sh->p_full[s], pp[s], sh, err)) return false;
+            pp[s] ^= 1;
+            if (!wait(&sh->v_full[vs], vp, sh, err)) return false;
+            fence_async_proxy();
+            tc_fence_after();
+            const uint32_t va = v_tiles + vs * R::kBytes;
+#pragma unroll
+            for (int i = 0; i < kTileKeys / 16; ++i)
+                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, v_desc(va + i * 2048), g.desc_pv, j >= 2 || i > 0);
+            umma_commit(&sh->pv_done[s]);
+            if (!two || s) {
+                umma_commit(&sh->v_empty[vs]);
+                if (++vs == R::kV) vs = 0, vp ^= 1;
+            }
+            if (j + 2 < steps && !scores(j + 2)) return false;
+        }
+    }
+    return true;
+}
+
+// ---- softmax ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+    uint32_t lo[16], hi[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        lo[i] = __float_as_uint(v[i]);
+        hi[i] = __float_as_uint(v[16 + i]);
+    }
+    tmem_st16(taddr, lo);
+    tmem_st16(taddr + 16, hi);
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int kDtype>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if (kDtype == SPEC_BF16) return pack_bf16x2(lo, hi);
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <int kDtype>
+__device__ __forceinline__ float number(uint32_t x, int which) {
+    if (kDtype == SPEC_BF16) return __uint_as_float(which ? x & 0xffff0000u : x << 16);
+    return __half2float(__ushort_as_half((unsigned short)(which ? x >> 16 : x & 0xffffu)));
+}
+
+// Which of the 32 keys from `first - len` on (in nodes of the tree; negative: the cache) the row of `node` sees.
+struct RowMask {
+    const uint32_t *words;             // null: a chain
+    int n_words, nodes, node;
+    __device__ uint32_t word(int i) const { return i < 0 ? 0xffffffffu : i < n_words ? words[i] : 0u; }
+    __device__ uint32_t bits(int first) const {
+        uint32_t m = 0xffffffffu;
+        int end = nodes;
+        if (words != nullptr) m = __funnelshift_r(word(first >> 5), word((first >> 5) + 1), first & 31);
+        else end = min(nodes, node + 1);
+        const int keep = end - first;
+        return keep >= 32 ? m : keep <= 0 ? 0u : m & ((1u << keep) - 1);
+    }
+};
+
+struct Row {
+    float top;                         // running maximum (times scale log2 e) that exponents are taken against
+    float sum;
+};
+
+// One tile of a row: probabilities in place of the scores.  The maximum follows the tiles lazily: probabilities are taken against an
+// older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
+// saves nearly every pass over the accumulated output (a pass waits for the products of the tile before).
+template <int kDtype, int kHalves, bool kMasked>
+__device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
+                                             uint64_t *pv_done, uint32_t pv_parity, const RowMask &mask, int key0, Row &row) {
+    float x[32];
+    float top = -INFINITY;
+    uint32_t seen[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        tmem_ld32(s_addr + c * 32, x);
+        if (kMasked) seen[c] = mask.bits(key0 + c * 32);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float y = kMasked && !(seen[c] >> i & 1) ? -INFINITY : x[i];
+            top = fmaxf(top, y);
+        }
+    }
+    top = top == -INFINITY ? top : top * g.scale_log2;
+    float shrink = 1.f;
+    if (first) {
+        row.top = top;
+    } else if (top > row.top + kRescaleAbove) {
+        shrink = ex2_approx(row.top - top);
+        row.top = top;
+    }
+    if (__any_sync(0xffffffffu, shrink != 1.f)) {
+        if (!warp_wait(pv_done, pv_parity, sh, g.a.err_word)) return false;
+        tc_fence_after();
+        row.sum *= shrink;
+#pragma unroll
+        for (int c = 0; c < 2 * kHalves; ++c) {
+            tmem_ld32(o_addr + c * 32, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] *= shrink;
+            tmem_st32(o_addr + c * 32, x);
+        }
+    }
+    const float base = row.top == -INFINITY ? 0.f : row.top;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        tmem_ld32(s_addr + c * 32, x);
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            float lo = ex2_approx(fmaf(x[i], g.scale_log2, -base)), hi = ex2_approx(fmaf(x[i + 1], g.scale_log2, -base));
+            if (kMasked) {
+                lo = seen[c] >> i & 1 ? lo : 0.f;
+                hi = seen[c] >> (i + 1) & 1 ? hi : 0.f;
+            }
+            sum[i / 2 % 4] += lo + hi;
+            p[i / 2] = pack2<kDtype>(lo, hi);
+        }
+        tmem_st16(s_addr + c * 16, p);
+    }
+    row.sum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    tmem_wait_st();
+    return true;
+}
+
+// What load_role kept out of the products: values that are not finite, of the nodes that the row sees, are added to the row's
+// result in memory, which its own thread has just written (columns col0 .. col0 + 31).
+template <int kDtype>
+__device__ __noinline__ void add_not_finite(const spec_tree_attention_t &a, const Unit &u, const RowMask &mask, int col0,
+                                            uint16_t *out, float *part) {
+    const int first = max(u.t0 * kTileKeys - u.len, 0), end = min(u.t1 * kTileKeys - u.len, u.nodes);
+    for (int n = first; n < end; ++n) {
+        if (!(mask.bits(n) & 1)) continue;
+        const uint16_t *v = (const uint16_t *)a.v + u.b * a.v_stride[0] + n * a.v_stride[1] + u.head * a.v_stride[2];
+        for (int i = col0; i < min(col0 + 32, a.D); ++i) {
+            const float x = number<kDtype>(v[i], 0);
+            if (fabsf(x) < INFINITY) continue;
+            if (part != nullptr) part[i] += x;
+            else out[i] = (uint16_t)pack2<kDtype>(number<kDtype>(out[i], 0) + x, 0.f);
+        }
+    }
+}
+
+// A barrier of the softmax threads whose wait is bounded like the others.
+__device__ __forceinline__ bool softmax_meet(Shared *sh, uint32_t &parity, int32_t *err) {
+    tc_fence_before();
+    mbar_arrive(&sh->meet);
+    if (!warp_wait(&sh->meet, parity, sh, err)) return false;
+    tc_fence_after();
+    parity ^= 1;
+    return true;
+}
+
+template <int kDtype, int kHalves>
+__device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
+    const spec_tree_attention_t &a = g.a;
+    const int stream = threadIdx.x >> 7, lane_row = threadIdx.x & 127;
+    const uint32_t lanes = sh->tmem_base + ((uint32_t)(lane_row & ~31) << 16);
+    const uint32_t s_addr = lanes + stream * 128;
+    uint32_t steps_done = 0, meet = 0;                   // steps of this stream over all units; parity
+    Walk walk(g, sh);
+    Unit u;
+    while (walk.next(g, u)) {
+        const bool two = u.two_tiles();
+        const int r = two ? stream * kTileRows + lane_row : lane_row;
+        const bool active = (r & ~31) < u.rows;          // of the warp
+        const int node = (u.row0 + min(r, u.rows - 1)) / g.group, head = u.row0 + r - node * g.group;
+        const int n_words = (a.T + 31) / 32;
+        const RowMask mask = {a.mask == nullptr ? nullptr : a.mask + ((size_t)u.b * a.T + node) * n_words, n_words, u.nodes, node};
+        Row row = {-INFINITY, 0.f};
+        bool first = true;
+        for (int t = two ? u.t0 : u.t0 + stream; t < u.t1; t += two ? 1 : 2) {
+            if (!warp_wait(&sh->s_full[stream], steps_done & 1, sh, a.err_word)) return false;
+            tc_fence_after();
+            if (active) {
+                const int key0 = t * kTileKeys - u.len;
+                const uint32_t o_addr = lanes + 256 + stream * 128;
+                const bool ok = key0 + kTileKeys > 0
+                                    ? softmax_tile<kDtype, kHalves, true>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
+                                                                          (steps_done - 1) & 1, mask, key0, row)
+                                    : softmax_tile<kDtype, kHalves, false>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
+                                                                           (steps_done - 1) & 1, mask, key0, row);
+                if (!ok) return false;
+            }
+            first = false;
+            tc_fence_before();
+            mbar_arrive(&sh->p_full[stream]);
+            ++steps_done;
+        }
+        if (!first && !warp_wait(&sh->pv_done[stream], (steps_done - 1) & 1, sh, a.err_word)) return false;
+        // the two streams of one query tile are joined: each warp group takes every other 32 columns
+        float w[2] = {1.f, 0.f};
+        if (!two) {
+            sh->stat[stream][lane_row][0] = row.top;
+            sh->stat[stream][lane_row][1] = row.sum;
+            if (!softmax_meet(sh, meet, a.err_word)) return false;
+            const float top0 = sh->stat[0][lane_row][0], top1 = sh->stat[1][lane_row][0];
+            const float top = fmaxf(top0, top1), base = top == -INFINITY ? 0.f : top;
+            w[0] = ex2_approx(top0 - base);
+            w[1] = ex2_approx(top1 - base);
+            row.top = top;
+            row.sum = sh->stat[0][lane_row][1] * w[0] + sh->stat[1][lane_row][1] * w[1];
+        }
+        tc_fence_after();
+        const bool join = !two && u.t1 - u.t0 > 1, bad = sh->not_finite[u.index % kUnitFlags] != 0;
+        if (active) {
+            const float inv = row.sum == 0.f ? 0.f : 1.f / row.sum;
+            const float lse = row.sum == 0.f ? -INFINITY : row.top * kLn2 + logf(row.sum);
+            uint16_t *out = (uint16_t *)a.out + u.b * a.out_stride[0] + node * a.out_stride[1] +
+                            (u.head * g.group + head) * a.out_stride[2];
+            const size_t part = ((size_t)(2 * blockIdx.x + (u.index ? 1 : 0))) * g.part_rows + r;
+#pragma unroll 1
+            for (int c = two ? 0 : stream; c * 32 < a.D; c += two ? 1 : 2) {
+                float o[32];
+                tmem_ld32(lanes + 256 + (two ? stream * 128 : 0) + c * 32, o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= w[0];
+                if (join) {
+                    float o1[32];
+                    tmem_ld32(lanes + 384 + c * 32, o1);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = fmaf(o1[i], w[1], o[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    if (r >= u.rows || c * 32 + i >= a.D) continue;
+                    if (u.whole()) {
+                        uint4 y;
+                        y.x = pack2<kDtype>(o[i] * inv, o[i + 1] * inv);
+                        y.y = pack2<kDtype>(o[i + 2] * inv, o[i + 3] * inv);
+                        y.z = pack2<kDtype>(o[i + 4] * inv, o[i + 5] * inv);
+                        y.w = pack2<kDtype>(o[i + 6] * inv, o[i + 7] * inv);
+                        *(uint4 *)(out + c * 32 + i) = y;
+                    } else {
+                        float4 *y = (float4 *)(g.part_out + part * a.D + c * 32 + i);
+                        y[0] = make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+                        y[1] = make_float4(o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv);
+                    }
+                }
+                if (bad && r < u.rows) add_not_finite<kDtype>(a, u, mask, c * 32, out, u.whole() ? nullptr : g.part_out + part * a.D);
+                __syncwarp();
+            }
+            if (r < u.rows && (two || stream == 0)) {
+                if (!u.whole()) g.part_lse[part] = lse;
+                else if (a.lse != nullptr) a.lse[((size_t)u.b * a.T + node) * a.Hq + u.head * g.group + head] = lse;
+            }
+        }
+        if (!softmax_meet(sh, meet, a.err_word)) return false;       // nobody writes O, stat or the flag while somebody may still read them
+        if (threadIdx.x == 0) sh->not_finite[u.index % kUnitFlags] = 0;
+    }
+    return true;
+}
+
+template <int kDtype, int kHalves>
+__global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ AttnArgs g) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    using R = Ring<kHalves>;
+    const uint32_t q_tiles = smem_u32(smem), k_tiles = q_tiles + R::kQ * R::kBytes, v_tiles = k_tiles + R::kK * R::kBytes;
+    Shared *sh = (Shared *)(smem + (R::kQ + R::kK + R::kV) * R::kBytes);
+    const int warp = threadIdx.x >> 5;
+    griddep_launch();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh->q_full[i], kLoadThreads);
+            mbar_init(&sh->q_empty[i], 1);
+            mbar_init(&sh->s_full[i], 1);
+            mbar_init(&sh->p_full[i], kTileRows);
+            mbar_init(&sh->pv_done[i], 1);
+        }
+        for (int i = 0; i < R::kK; ++i) {
+            mbar_init(&sh->k_full[i], kLoadThreads);
+            mbar_init(&sh->k_empty[i], 1);
+        }
+        for (int i = 0; i < R::kV; ++i) {
+            mbar_init(&sh->v_full[i], kLoadThreads);
+            mbar_init(&sh->v_empty[i], 1);
+        }
+        mbar_init(&sh->meet, kSoftmaxThreads);
+        mbar_init(&sh->drained, 1);
+        sh->abort_flag = 0;
+        for (int i = 0; i < kUnitFlags; ++i) sh->not_finite[i] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                     "r"((uint32_t)kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    griddep_wait();
+    if (warp == 1) {
+        const long long tiles = all_tiles(g, blockIdx.x == 0);
+        const long long pos = cta_start(tiles, blockIdx.x, gridDim.x), end = cta_start(tiles, blockIdx.x + 1, gridDim.x);
+        long long off = 0;
+        const int b = pos < end ? find_tile(g, pos, off) : g.a.B;
+        if ((threadIdx.x & 31) == 0) {
+            sh->start_b = b;
+            sh->start_off = off;
+            sh->pos = pos;
+            sh->end = end;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp < 8) {
+        softmax_role<kDtype, kHalves>(g, sh);
+    } else if (warp == 8) {
+        if (tc::elect_one()) {
+            mma_role<kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
+            umma_commit(&sh->drained);                   // what was issued ends before TMEM and shared memory go
+            for (uint32_t it = 0; it < tc::kSpinMax && !mbar_try_wait(&sh->drained, 0); ++it) {}
+        }
+        __syncwarp();
+    } else {
+        load_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh->tmem_base), "r"((uint32_t)kTmemCols) : "memory");
+    }
+}
+
+// ---- joining the parts of a unit -------------------------------------------------------------------------------------
+// A unit is split where the first tile of some CTA lies inside it.  Block c looks at the first tile of CTA c + 1 and joins the
+// unit that holds it, if that is the first such border in the unit; blockIdx.y takes kJoinRows of its rows, a warp per row.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 16;
+
+template <int kDtype>
+__global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid_constant__ AttnArgs g, int ctas) {
+    const spec_tree_attention_t &a = g.a;
     griddep_launch();
     griddep_wait();
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, t = threadIdx.x, g = h / (a.Hq / a.Hkv);
-    const int cap = (int)min((long long)a.max_pages * a.page_size, (long long)INT_MAX);
-    const int len_in = a.seq_len[b], nodes_in = a.n_nodes ? a.n_nodes[b] : a.T;
-    const int len = min(max(len_in, 0), cap), nodes = min(max(nodes_in, 0), a.T);
-    if (t == 0 && (len != len_in || nodes != nodes_in)) report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
-    if (i >= nodes) return;
-    const uint16_t *qr = (const uint16_t *)a.q + b * a.q_stride[0] + i * a.q_stride[1] + h * a.q_stride[2];
-    if (t < a.D) q[t] = to_float<kDtype>(qr[t]);
-    float top = -INFINITY, total = 0.f, acc = 0.f;
-    for (int k0 = 0; k0 < len + nodes; k0 += kSimpleThreads) {
-        __syncthreads();
-        const int key = k0 + t;
-        const uint16_t *kr = nullptr, *vr = nullptr;
-        if (key < len) {
-            const int page = key / a.page_size, off = key - page * a.page_size, id = a.block_table[b * a.table_stride + page];
-            if (id >= 0 && id < a.n_pages) {
-                kr = (const uint16_t *)a.k_cache + id * a.kc_stride[0] + off * a.kc_stride[1] + g * a.kc_stride[2];
-                vr = (const uint16_t *)a.v_cache + id * a.vc_stride[0] + off * a.vc_stride[1] + g * a.vc_stride[2];
-            } else {
-                report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x;
+    const long long tiles = all_tiles(g, false), border = cta_start(tiles, c + 1, ctas), mine = cta_start(tiles, c, ctas);
+    if (mine == border || border >= tiles) return;
+    long long off;
+    const int b = find_tile(g, border, off);
+    if (b >= a.B) return;
+    const Seq s = seq_of(g, b, false);
+    const int unit = (int)(off / s.tiles), inside = (int)(off - (long long)unit * s.tiles);
+    const long long first = border - inside, last = first + s.tiles;
+    if (inside == 0 || mine > first) return;
+    const int blocks = s.units / a.Hkv, head = unit / blocks, row0 = (unit - head * blocks) * 2 * kTileRows;
+    const int rows = min(s.nodes * g.group - row0, 2 * kTileRows);
+    int parts = 1;                       // CTAs c .. c + parts - 1 hold parts; some may have no tile at all
+    while (c + parts < ctas && cta_start(tiles, c + parts, ctas) < last) ++parts;
+    for (int r = blockIdx.y * kJoinRows + warp; r < min(rows, ((int)blockIdx.y + 1) * kJoinRows); r += kJoinThreads / 32) {
+        const int col = lane * 4;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = -INFINITY, sum = 0.f;
+        for (int i = 0; i < parts; ++i) {
+            const long long begin = cta_start(tiles, c + i, ctas);
+            if (begin == cta_start(tiles, c + i + 1, ctas)) continue;
+            const size_t part = (size_t)(2 * (c + i) + (begin < first ? 1 : 0)) * g.part_rows + r;
+            const float lse = g.part_lse[part];
+            if (lse == -INFINITY) continue;
+            const float next = fmaxf(top, lse), keep = __expf(top - next), take = __expf(lse - next);
+            top = next;
+            sum = sum * keep + take;
+            if (col < a.D) {
+                const float4 o = *(const float4 *)(g.part_out + part * a.D + col);
+                // (a part whose weight is nothing still carries what is not finite)
+                acc.x = acc.x * keep + (fabsf(o.x) < INFINITY ? o.x * take : o.x);
+                acc.y = acc.y * keep + (fabsf(o.y) < INFINITY ? o.y * take : o.y);
+                acc.z = acc.z * keep + (fabsf(o.z) < INFINITY ? o.z * take : o.z);
+                acc.w = acc.w * keep + (fabsf(o.w) < INFINITY ? o.w * take : o.w);
             }
-        } else if (key < len + nodes) {
-            const int n = key - len;
-            kr = (const uint16_t *)a.k + b * a.k_stride[0] + n * a.k_stride[1] + g * a.k_stride[2];
-            vr = (const uint16_t *)a.v + b * a.v_stride[0] + n * a.v_stride[1] + g * a.v_stride[2];
         }
-        bool sees = key < len;
-        if (key >= len && key < len + nodes) {
-            const int n = key - len;
-            sees = a.mask ? a.mask[((size_t)b * a.T + i) * ((a.T + 31) / 32) + (n >> 5)] >> (n & 31) & 1 : n <= i;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int node = (row0 + r) / g.group, h = head * g.group + row0 + r - node * g.group;
+        if (col < a.D) {
+            uint2 y;
+            y.x = pack2<kDtype>(acc.x * inv, acc.y * inv);
+            y.y = pack2<kDtype>(acc.z * inv, acc.w * inv);
+            *(uint2 *)((uint16_t *)a.out + b * a.out_stride[0] + node * a.out_stride[1] + h * a.out_stride[2] + col) = y;
         }
-        float s = -INFINITY;
-        if (sees) {
-            s = 0.f;
-            if (kr)
-                for (int d = 0; d < a.D; ++d) s += q[d] * to_float<kDtype>(kr[d]);
-            s *= a.scale;
-        }
-        const float m = fmaxf(top, block_reduce<true>(s, part));
-        const float w = sees ? expf(s - m) : 0.f;
-        p[t] = w;
-        val[t] = sees ? vr : nullptr;
-        const float keep = m == -INFINITY ? 1.f : expf(top - m);
-        total = total * keep + block_reduce<false>(w, part);
-        acc *= keep;
-        top = m;
-        if (t < a.D)
-            for (int j = 0; j < min(kSimpleThreads, len + nodes - k0); ++j)
-                if (val[j]) acc += p[j] * to_float<kDtype>(val[j][t]);
+        if (lane == 0 && a.lse != nullptr)
+            a.lse[((size_t)b * a.T + node) * a.Hq + h] = sum == 0.f ? -INFINITY : top + logf(sum);
     }
-    uint16_t *out = (uint16_t *)a.out + b * a.out_stride[0] + i * a.out_stride[1] + h * a.out_stride[2];
-    if (t < a.D) out[t] = from_float<kDtype>(total == 0.f ? 0.f : acc / total);
-    if (t == 0 && a.lse) a.lse[((size_t)b * a.T + i) * a.Hq + h] = total == 0.f ? -INFINITY : top + logf(total);
+}
+
+bool strides_ok(const int64_t (&s)[3]) { return s[0] >= 0 && s[1] >= 0 && s[2] >= 0 && !(s[0] % 8) && !(s[1] % 8) && !(s[2] % 8); }
+
+int check_shape(int B, int T, int Hq, int Hkv, int D) {
+    if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || D <= 0) return SPEC_ERR_INVALID_ARG;
+    if (D % 8 != 0 || D > 128 || Hq % Hkv != 0 || T > SPEC_MAX_TREE_NODES || Hq > 65535 || B > (1 << 20)) return SPEC_ERR_SHAPE;
+    return SPEC_OK;
+}
+
+int part_rows(int T, int Hq, int Hkv) {
+    const long long rows = (long long)T * (Hq / Hkv);
+    return rows < 2 * kTileRows ? (int)rows : 2 * kTileRows;
+}
+size_t part_lse_bytes(int T, int Hq, int Hkv) {
+    return ((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * 4 + kWsAlign - 1) / kWsAlign * kWsAlign;
+}
+
+template <int kDtype, int kHalves>
+int launch(const AttnArgs &g, cudaStream_t st) {
+    const int ctas = num_sms();
+    auto kernel = tree_attention_kernel<kDtype, kHalves>;
+    SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<kHalves>()));
+    SPEC_CUDA_TRY(launch_pdl(kernel, dim3(ctas), dim3(kThreads), smem_bytes<kHalves>(), st, g));
+    SPEC_CUDA_TRY(launch_pdl(tree_combine_kernel<kDtype>, dim3(ctas - 1, (g.part_rows + kJoinRows - 1) / kJoinRows),
+                             dim3(kJoinThreads), 0, st, g, ctas));
+    return SPEC_OK;
 }
 
 }  // namespace
@@ -101,23 +865,11 @@ __global__ void __launch_bounds__(kSimpleThreads) tree_attention_kernel(const sp
 
 using namespace spec;
 
-namespace {
-
-bool strides_ok(const int64_t (&s)[3]) { return s[0] >= 0 && s[1] >= 0 && s[2] >= 0 && !(s[0] % 8) && !(s[1] % 8) && !(s[2] % 8); }
-
-int check_shape(int B, int T, int Hq, int Hkv, int D) {
-    if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || D <= 0) return SPEC_ERR_INVALID_ARG;
-    if (D % 8 != 0 || D > 128 || Hq % Hkv != 0 || T > SPEC_MAX_TREE_NODES || B > 65535 || Hq > 65535) return SPEC_ERR_SHAPE;
-    return SPEC_OK;
-}
-
-}  // namespace
-
 extern "C" {
 
 size_t spec_tree_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
     if (check_shape(B, T, Hq, Hkv, D) != SPEC_OK) return 0;
-    return kWsAlign;
+    return part_lse_bytes(T, Hq, Hkv) + ((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * D * 4 + kWsAlign - 1) / kWsAlign * kWsAlign;
 }
 
 int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t workspace_bytes, void *cuda_stream) {
@@ -126,7 +878,7 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_INVALID_ARG;
     const int rc = check_shape(a->B, a->T, a->Hq, a->Hkv, a->D);
     if (rc != SPEC_OK) return rc;
-    if (a->page_size <= 0 || a->n_pages <= 0 || a->max_pages <= 0 || !(a->scale == a->scale)) return SPEC_ERR_INVALID_ARG;
+    if (a->page_size <= 0 || a->n_pages <= 0 || a->max_pages <= 0 || !(fabsf(a->scale) < INFINITY)) return SPEC_ERR_INVALID_ARG;
     if (a->table_stride < a->max_pages) return SPEC_ERR_SHAPE;
     const void *ptrs[] = {a->q, a->k, a->v, a->k_cache, a->v_cache, a->out};
     for (const void *p : ptrs)
@@ -137,11 +889,21 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     if (!workspace || ((uintptr_t)workspace % kWsAlign) != 0 ||
         workspace_bytes < spec_tree_attention_workspace_bytes(a->B, a->T, a->Hq, a->Hkv, a->D))
         return SPEC_ERR_WORKSPACE;
-    const dim3 grid(a->Hq, a->T, a->B);
+    AttnArgs g;
+    g.a = *a;
+    g.group = a->Hq / a->Hkv;
+    g.scale_log2 = fabsf(a->scale) * kLog2e;
+    const bool bf16 = a->dtype == SPEC_BF16;
+    const uint32_t type = bf16 ? 1u << 7 | 1u << 10 : 0u;              // A and B: bf16 or fp16
+    const uint32_t common = 1u << 4 | type | (uint32_t)(kTileRows >> 4) << 24;
+    g.desc_qk = common | (uint32_t)(kTileKeys >> 3) << 17 | (a->scale < 0.f ? 1u << 13 : 0u);       // a negative scale negates Q
+    g.desc_pv = common | (uint32_t)((a->D + 15) / 16 * 2) << 17 | 1u << 16;                         // V is MN-major
+    g.part_rows = part_rows(a->T, a->Hq, a->Hkv);
+    g.part_lse = (float *)workspace;
+    g.part_out = (float *)((char *)workspace + part_lse_bytes(a->T, a->Hq, a->Hkv));
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (a->dtype == SPEC_BF16) SPEC_CUDA_TRY(launch_pdl(tree_attention_kernel<SPEC_BF16>, grid, dim3(kSimpleThreads), 0, st, *a));
-    else SPEC_CUDA_TRY(launch_pdl(tree_attention_kernel<SPEC_F16>, grid, dim3(kSimpleThreads), 0, st, *a));
-    return SPEC_OK;
+    if (a->D <= 64) return bf16 ? launch<SPEC_BF16, 1>(g, st) : launch<SPEC_F16, 1>(g, st);
+    return bf16 ? launch<SPEC_BF16, 2>(g, st) : launch<SPEC_F16, 2>(g, st);
 }
 
 }  // extern "C"
