@@ -7,11 +7,12 @@
 // has to itself is written straight to `out`; of the others every CTA leaves its rows, normalised, with their log-sum-exp in
 // the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
 //
-// Roles of a CTA (13 warps):
+// Roles of a CTA (16 warps):
 //   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
 //                   TMEM in place of the scores, results
 //   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 128], O += P V, P read from TMEM
-//   warps 9-12      gather rows of Q, K and V with 16-byte asynchronous copies (pages of any size, any strides; rows that do
+//   warps 9-11      nothing (registers are given away by groups of four warps)
+//   warps 12-15     gather rows of Q, K and V with 16-byte asynchronous copies (pages of any size, any strides; rows that do
 //                   not exist read as zeros) into 128-byte-swizzled tiles
 // Two streams keep the tensor cores busy while a softmax runs.  Units of more than 128 rows have a stream per 128 rows, both on the
 // same tile of keys; smaller ones give their tiles to the streams in turn, and the two results are joined at the end.
@@ -42,8 +43,11 @@ constexpr int kTileRows = 128;
 constexpr int kHalfBytes = kTileKeys * 128;     // 64 columns of a tile of 128 rows
 constexpr int kSoftmaxThreads = 256;
 constexpr int kLoadThreads = 128;
-constexpr int kFirstLoader = kSoftmaxThreads + 32;
+constexpr int kFirstLoader = kSoftmaxThreads + 128;
 constexpr int kThreads = kFirstLoader + kLoadThreads;
+// Registers of a thread after the roles have parted; 2 * 128 * (192 + 64) is what the launch has (512 threads of 128).  (All that the
+// roles call is inlined: around a call the compiler does not go beyond the launch's 128.)
+constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
 constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns each
 constexpr int kUnitFlags = 8;
 constexpr float kRescaleAbove = 8.f;            // see softmax_tile
@@ -84,7 +88,7 @@ struct AttnArgs {
     int part_rows;
 };
 
-__device__ __noinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
+__device__ __forceinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
     for (uint32_t it = 0; it < tc::kSpinMax; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
         if (it > tc::kSpinFast) {
@@ -464,16 +468,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
-    uint32_t lo[16], hi[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        lo[i] = __float_as_uint(v[i]);
-        hi[i] = __float_as_uint(v[16 + i]);
-    }
-    tmem_st16(taddr, lo);
-    tmem_st16(taddr + 16, hi);
-}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <int kDtype>
@@ -509,25 +503,61 @@ struct Row {
     float sum;
 };
 
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[128], int at) {
+#define V(i) "=f"(v[at + i])
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : V(0), V(1), V(2), V(3), V(4), V(5), V(6), V(7), V(8), V(9), V(10), V(11), V(12), V(13), V(14), V(15), V(16), V(17),
+          V(18), V(19), V(20), V(21), V(22), V(23), V(24), V(25), V(26), V(27), V(28), V(29), V(30), V(31)
+        : "r"(taddr) : "memory");
+#undef V
+}
+// 128 columns: the four loads are in flight together.  Nothing may use a register before the wait, so each passes through a
+// statement behind it.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 32) tmem_ld32_async(taddr + c, v, c);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int c = 0; c < 128; c += 8)
+        asm volatile("" : "+f"(v[c]), "+f"(v[c + 1]), "+f"(v[c + 2]), "+f"(v[c + 3]), "+f"(v[c + 4]), "+f"(v[c + 5]), "+f"(v[c + 6]),
+                          "+f"(v[c + 7]));
+}
+
+// Two lanes of fp32 arithmetic in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*(unsigned long long *)&a), "l"(*(unsigned long long *)&b), "l"(*(unsigned long long *)&c));
+    return *(float2 *)&r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*(unsigned long long *)&a), "l"(*(unsigned long long *)&b));
+    return *(float2 *)&r;
+}
+
 // One tile of a row: probabilities in place of the scores.  The maximum follows the tiles lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
 // saves nearly every pass over the accumulated output (a pass waits for the products of the tile before).
 template <int kDtype, int kHalves, bool kMasked>
 __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
-                                             uint64_t *pv_done, uint32_t pv_parity, const RowMask &mask, int key0, Row &row) {
-    float x[32];
-    float top = -INFINITY;
-    uint32_t seen[4];
+                                             uint64_t *pv_done, uint32_t pv_parity, const uint32_t (&seen)[4], Row &row) {
+    float x[128];
+    tmem_ld128(s_addr, x);
+    float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        tmem_ld32(s_addr + c * 32, x);
-        if (kMasked) seen[c] = mask.bits(key0 + c * 32);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float y = kMasked && !(seen[c] >> i & 1) ? -INFINITY : x[i];
-            top = fmaxf(top, y);
+    for (int i = 0; i < 128; i += 2) {
+        if (kMasked) {
+            if (!(seen[i >> 5] >> (i & 31) & 1)) x[i] = -INFINITY;
+            if (!(seen[i >> 5] >> (i & 31) & 2)) x[i + 1] = -INFINITY;
         }
+        top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
     }
+    float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
     top = top == -INFINITY ? top : top * g.scale_log2;
     float shrink = 1.f;
     if (first) {
@@ -540,33 +570,38 @@ __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint
         if (!warp_wait(pv_done, pv_parity, sh, g.a.err_word)) return false;
         tc_fence_after();
         row.sum *= shrink;
+#pragma unroll 1
+        for (int c = 0; c < 4 * kHalves; ++c) {
+            float o[16];
+            uint32_t r[16];
+            tc::tmem_ld16(o_addr + c * 16, o);
 #pragma unroll
-        for (int c = 0; c < 2 * kHalves; ++c) {
-            tmem_ld32(o_addr + c * 32, x);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] *= shrink;
-            tmem_st32(o_addr + c * 32, x);
+            for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(o[i] * shrink);
+            tmem_st16(o_addr + c * 16, r);
         }
     }
     const float base = row.top == -INFINITY ? 0.f : row.top;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const float2 scale = make_float2(g.scale_log2, g.scale_log2), minus = make_float2(-base, -base);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-        tmem_ld32(s_addr + c * 32, x);
         uint32_t p[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            float lo = ex2_approx(fmaf(x[i], g.scale_log2, -base)), hi = ex2_approx(fmaf(x[i + 1], g.scale_log2, -base));
-            if (kMasked) {
-                lo = seen[c] >> i & 1 ? lo : 0.f;
-                hi = seen[c] >> (i + 1) & 1 ? hi : 0.f;
+            float2 y = fma2(make_float2(x[c * 32 + i], x[c * 32 + i + 1]), scale, minus);
+            y.x = ex2_approx(y.x);
+            y.y = ex2_approx(y.y);
+            if (kMasked) {               // (minus infinity times a scale of zero is not minus infinity)
+                if (!(seen[c] >> i & 1)) y.x = 0.f;
+                if (!(seen[c] >> i & 2)) y.y = 0.f;
             }
-            sum[i / 2 % 4] += lo + hi;
-            p[i / 2] = pack2<kDtype>(lo, hi);
+            sum[i / 2 % 2] = add2(sum[i / 2 % 2], y);
+            p[i / 2] = pack2<kDtype>(y.x, y.y);
         }
         tmem_st16(s_addr + c * 16, p);
     }
-    row.sum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    sum[0] = add2(sum[0], sum[1]);
+    row.sum += sum[0].x + sum[0].y;
     tmem_wait_st();
     return true;
 }
@@ -574,7 +609,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint
 // What load_role kept out of the products: values that are not finite, of the nodes that the row sees, are added to the row's
 // result in memory, which its own thread has just written (columns col0 .. col0 + 31).
 template <int kDtype>
-__device__ __noinline__ void add_not_finite(const spec_tree_attention_t &a, const Unit &u, const RowMask &mask, int col0,
+__device__ __forceinline__ void add_not_finite(const spec_tree_attention_t &a, const Unit &u, const RowMask &mask, int col0,
                                             uint16_t *out, float *part) {
     const int first = max(u.t0 * kTileKeys - u.len, 0), end = min(u.t1 * kTileKeys - u.len, u.nodes);
     for (int n = first; n < end; ++n) {
@@ -618,16 +653,21 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
         Row row = {-INFINITY, 0.f};
         bool first = true;
         for (int t = two ? u.t0 : u.t0 + stream; t < u.t1; t += two ? 1 : 2) {
+            const int key0 = t * kTileKeys - u.len;
+            const bool masked = key0 + kTileKeys > 0;
+            uint32_t seen[4];
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) seen[c] = mask.bits(key0 + c * 32);
+            }
             if (!warp_wait(&sh->s_full[stream], steps_done & 1, sh, a.err_word)) return false;
             tc_fence_after();
             if (active) {
-                const int key0 = t * kTileKeys - u.len;
-                const uint32_t o_addr = lanes + 256 + stream * 128;
-                const bool ok = key0 + kTileKeys > 0
-                                    ? softmax_tile<kDtype, kHalves, true>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
-                                                                          (steps_done - 1) & 1, mask, key0, row)
-                                    : softmax_tile<kDtype, kHalves, false>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
-                                                                           (steps_done - 1) & 1, mask, key0, row);
+                const uint32_t o_addr = lanes + 256 + stream * 128, parity = (steps_done - 1) & 1;
+                const bool ok = masked ? softmax_tile<kDtype, kHalves, true>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
+                                                                             parity, seen, row)
+                                       : softmax_tile<kDtype, kHalves, false>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
+                                                                              parity, seen, row);
                 if (!ok) return false;
             }
             first = false;
@@ -752,15 +792,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     __syncthreads();
     tc_fence_after();
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         softmax_role<kDtype, kHalves>(g, sh);
-    } else if (warp == 8) {
-        if (tc::elect_one()) {
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 8 && tc::elect_one()) {
             mma_role<kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
             umma_commit(&sh->drained);                   // what was issued ends before TMEM and shared memory go
             for (uint32_t it = 0; it < tc::kSpinMax && !mbar_try_wait(&sh->drained, 0); ++it) {}
         }
         __syncwarp();
     } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         load_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
         asm volatile("cp.async.wait_all;" ::: "memory");
     }
