@@ -12,8 +12,9 @@
 //                   TMEM in place of the scores, results
 //   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 128], O += P V, P read from TMEM
 //   warps 9-11      nothing (registers are given away by groups of four warps)
-//   warps 12-15     gather rows of Q, K and V with 16-byte asynchronous copies (pages of any size, any strides; rows that do
-//                   not exist read as zeros) into 128-byte-swizzled tiles
+//   warps 12-15     load tiles of Q, K and V, 128-byte-swizzled: tiles that lie in the cache as TMA boxes, a page (or 128 tokens of
+//                   one) by 64 columns each; the tile in which the cache ends and the tree begins, the tree, Q, and caches whose
+//                   pages do not tile 128 keys row by row with 16-byte asynchronous copies (rows that do not exist read as zeros)
 // Two streams keep the tensor cores busy while a softmax runs.  Units of more than 128 rows have a stream per 128 rows, both on the
 // same tile of keys; smaller ones give their tiles to the streams in turn, and the two results are joined at the end.
 #include <limits.h>
@@ -86,6 +87,9 @@ struct AttnArgs {
     float *part_out;          // [2 * CTAs][part_rows][D]
     float *part_lse;          // [2 * CTAs][part_rows]
     int part_rows;
+    int box_tokens;           // tokens of a TMA box, 0: the cache is not read by TMA (see cache_map)
+    int box_pieces;           // kTileKeys / box_tokens
+    CUtensorMap k_map, v_map; // the caches as (column, token, head, page)
 };
 
 __device__ __forceinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
@@ -290,6 +294,47 @@ __device__ __forceinline__ const uint16_t *row_of(KeyPlace p, int b, int head, c
     return nullptr;
 }
 
+// The boxes of a whole tile of the cache are dealt to the four loading warps: box i is piece i / kHalves of 128 / box_tokens,
+// columns 64 * (i % kHalves).  Lane l of a warp looks up the page of the warp's box l, a tile ahead.  Nothing here divides but where
+// a page holds several tiles: with a division per box and lookups that the copies wait for, four warps brought in 2.8 TB/s.
+constexpr int kMaxBoxes = 8;                             // of a warp: pages of 8 tokens, two halves
+template <int kHalves>
+__device__ __forceinline__ int box_page(const AttnArgs &g, const Unit &u, int tile, int warp, int lane) {
+    const spec_tree_attention_t &a = g.a;
+    const int piece = (warp + 4 * lane) / kHalves;
+    if (piece >= g.box_pieces) return 0;
+    const int index = a.page_size > kTileKeys ? tile / (a.page_size / kTileKeys) : tile * g.box_pieces + piece;
+    const int id = a.block_table[u.b * a.table_stride + index];
+    if (id >= 0 && id < a.n_pages) return id;
+    report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
+    return a.n_pages;                                    // behind the tensor: the box reads as zeros
+}
+template <int kHalves>
+__device__ __forceinline__ void load_boxes(const AttnArgs &g, const CUtensorMap *map, const Unit &u, int tile, int page, int warp,
+                                           uint32_t dst, uint64_t *bar) {
+    const int boxes = g.box_pieces * kHalves, bytes = g.box_tokens * 128;
+    const int token = g.a.page_size > kTileKeys ? tile % (g.a.page_size / kTileKeys) * kTileKeys : 0;
+    int id[kMaxBoxes];
+#pragma unroll
+    for (int i = 0; i < kMaxBoxes; ++i) id[i] = __shfl_sync(0xffffffffu, page, i);
+    if (tc::elect_one()) {
+        if (warp < boxes) tc::mbar_arrive_expect_tx(bar, (boxes - warp + 3) / 4 * bytes);
+        else mbar_arrive(bar);
+#pragma unroll
+        for (int i = 0; i < kMaxBoxes; ++i) {
+            const int box = warp + 4 * i, piece = box / kHalves, half = box % kHalves;
+            if (box >= boxes) break;
+            asm volatile(
+                "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                ::"r"(dst + half * kHalfBytes + piece * bytes), "l"((uint64_t)map), "r"(half * 64), "r"(token), "r"(u.head),
+                "r"(id[i]), "r"(smem_u32(bar)) : "memory");
+        }
+    } else {
+        mbar_arrive(bar);
+    }
+    __syncwarp();
+}
+
 // Is one of the eight numbers not finite?  (bf16 has eight exponent bits, fp16 five.)
 template <int kDtype>
 __device__ __forceinline__ uint32_t finite_or_zero(uint32_t x, bool &bad) {
@@ -326,20 +371,40 @@ __device__ void load_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint3
             arrive_when_copied(&sh->q_full[qs]);
             if (++qs == R::kQ) qs = 0, qp ^= 1;
         }
-        // K of a tile goes ahead of V of the tile before
-        KeyPlace here = key_place(a, u, u.t0 * kTileKeys + map.own_row()), before = here;
+        // K of a tile goes ahead of V of the tile before.  Tiles [t0, boxed) lie in the cache and come by TMA.
+        const int boxed = g.box_tokens ? min(u.t1, max(u.t0, u.len / kTileKeys)) : u.t0;
+        KeyPlace here, before;
+        int page = 0, page_before = 0;
+        auto look = [&](int t) {
+            if (t < boxed) page = box_page<kHalves>(g, u, t, map.warp, map.lane);
+            else if (t < u.t1) here = key_place(a, u, t * kTileKeys + map.own_row());
+        };
+        look(u.t0);
         for (int t = u.t0; t <= u.t1; ++t) {
-            KeyPlace ahead = here;
+            const KeyPlace now = here;
+            const int page_now = page;
             if (t < u.t1) {
-                if (t + 1 < u.t1) ahead = key_place(a, u, (t + 1) * kTileKeys + map.own_row());
+                look(t + 1);                             // (ahead of the wait)
                 if (!warp_wait(&sh->k_empty[ks], kp, sh, a.err_word)) return;
-                map.copy(k_tiles + ks * R::kBytes, row_of(here, u.b, u.head, a.k_cache, a.kc_stride, a.k, a.k_stride), a.D);
-                arrive_when_copied(&sh->k_full[ks]);
+                const uint32_t tile = k_tiles + ks * R::kBytes;
+                if (t < boxed) {
+                    load_boxes<kHalves>(g, &g.k_map, u, t, page_now, map.warp, tile, &sh->k_full[ks]);
+                } else {
+                    map.copy(tile, row_of(now, u.b, u.head, a.k_cache, a.kc_stride, a.k, a.k_stride), a.D);
+                    arrive_when_copied(&sh->k_full[ks]);
+                }
                 if (++ks == R::kK) ks = 0, kp ^= 1;
             }
             if (t > u.t0) {
                 if (!warp_wait(&sh->v_empty[vs], vp, sh, a.err_word)) return;
                 const uint32_t tile = v_tiles + vs * R::kBytes;
+                if (t - 1 < boxed) {
+                    load_boxes<kHalves>(g, &g.v_map, u, t - 1, page_before, map.warp, tile, &sh->v_full[vs]);
+                    if (++vs == R::kV) vs = 0, vp ^= 1;
+                    before = now;
+                    page_before = page_now;
+                    continue;
+                }
                 map.copy(tile, row_of(before, u.b, u.head, a.v_cache, a.vc_stride, a.v, a.v_stride), a.D);
                 const int key0 = (t - 1) * kTileKeys;
                 if (key0 + kTileKeys > u.len) {
@@ -371,8 +436,8 @@ __device__ void load_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint3
                 }
                 if (++vs == R::kV) vs = 0, vp ^= 1;
             }
-            before = here;
-            here = ahead;
+            before = now;
+            page_before = page_now;
         }
     }
 }
@@ -892,6 +957,31 @@ size_t part_lse_bytes(int T, int Hq, int Hkv) {
     return ((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * 4 + kWsAlign - 1) / kWsAlign * kWsAlign;
 }
 
+// The cache as a TMA tensor whose boxes are a page, or 128 tokens of one, by 64 columns of a head.  Pages have to tile 128 keys
+// or be tiled by them, in whole groups of 8 rows (the swizzle's period).  False: not such a cache, or strides that TMA does not take.
+bool cache_map(const spec_tree_attention_t &a, const void *base, const int64_t (&stride)[3], int box_tokens, CUtensorMap *map) {
+    static const auto encode = []() -> decltype(&cuTensorMapEncodeTiled) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return (decltype(&cuTensorMapEncodeTiled))fn;
+    }();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.page_size, (cuuint64_t)a.Hkv, (cuuint64_t)a.n_pages};
+    cuuint64_t bytes[3];
+    const int64_t strides[3] = {stride[1], stride[2], stride[0]};
+    for (int i = 0; i < 3; ++i) {
+        if (strides[i] == 0 && dims[i + 1] > 1) return false;
+        bytes[i] = strides[i] ? (cuuint64_t)strides[i] * 2 : ((cuuint64_t)a.D * 2 + 15) / 16 * 16;
+    }
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, 1, 1}, step[4] = {1, 1, 1, 1};
+    return encode(map, a.dtype == SPEC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                  const_cast<void *>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int kDtype, int kHalves>
 int launch(const AttnArgs &g, cudaStream_t st) {
     const int ctas = num_sms();
@@ -944,6 +1034,11 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     g.part_rows = part_rows(a->T, a->Hq, a->Hkv);
     g.part_lse = (float *)workspace;
     g.part_out = (float *)((char *)workspace + part_lse_bytes(a->T, a->Hq, a->Hkv));
+    g.box_tokens = a->page_size % 8 ? 0 : kTileKeys % a->page_size == 0 ? a->page_size : a->page_size % kTileKeys == 0 ? kTileKeys : 0;
+    if (g.box_tokens && (!cache_map(*a, a->k_cache, a->kc_stride, g.box_tokens, &g.k_map) ||
+                         !cache_map(*a, a->v_cache, a->vc_stride, g.box_tokens, &g.v_map)))
+        g.box_tokens = 0;
+    g.box_pieces = g.box_tokens ? kTileKeys / g.box_tokens : 0;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (a->D <= 64) return bf16 ? launch<SPEC_BF16, 1>(g, st) : launch<SPEC_F16, 1>(g, st);
     return bf16 ? launch<SPEC_BF16, 2>(g, st) : launch<SPEC_F16, 2>(g, st);
