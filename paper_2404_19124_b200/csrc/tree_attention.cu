@@ -174,7 +174,10 @@ __device__ int find_tile(const AttnArgs &g, long long pos, long long &off) {
     return g.a.B;
 }
 
-__device__ __forceinline__ long long cta_start(long long tiles, int cta, int ctas) { return tiles * cta / ctas; }
+__device__ __forceinline__ long long cta_start(long long tiles, int cta, int ctas) {
+    return (unsigned long long)tiles < 0x1000000ull ? (unsigned)tiles * (unsigned)cta / (unsigned)ctas
+                                                     : (unsigned long long)tiles * (unsigned)cta / (unsigned)ctas;
+}
 
 // A unit's tiles [t0, t1) that this CTA has.
 struct Unit {
@@ -489,10 +492,14 @@ __device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32
             if (j < 2 && !wait(&sh->q_full[q], s ? qp1 : qp0, sh, err)) return false;
             if (!wait(&sh->k_full[ks], kp, sh, err)) return false;
             fence_async_proxy();
-            const uint32_t qa = q_tiles + q * R::kBytes, ka = k_tiles + ks * R::kBytes;
-            for (int i = 0; i < k_steps; ++i) {
-                const uint32_t off = (i >> 2) * kHalfBytes + (i & 3) * 32;
-                mma_ss(tmem + s * 128, tc::make_smem_desc(qa + off), tc::make_smem_desc(ka + off), g.desc_qk, i > 0);
+            // (Unrolled, with descriptors that differ by constants: a loop that builds them took 140 cycles an MMA, twice its time.)
+            const uint64_t qd = tc::make_smem_desc(q_tiles + q * R::kBytes), kd = tc::make_smem_desc(k_tiles + ks * R::kBytes);
+            const uint32_t d = tmem + s * 128, desc = g.desc_qk;
+#pragma unroll
+            for (int i = 0; i < 4 * kHalves; ++i) {
+                constexpr int kHalf = kHalfBytes >> 4;
+                const int off = (i >> 2) * kHalf + (i & 3) * 2;
+                if (i < k_steps) mma_ss(d, qd + off, kd + off, desc, i > 0);
             }
             umma_commit(&sh->s_full[s]);
             if (!two || s) {
@@ -511,10 +518,10 @@ __device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32
             if (!wait(&sh->v_full[vs], vp, sh, err)) return false;
             fence_async_proxy();
             tc_fence_after();
-            const uint32_t va = v_tiles + vs * R::kBytes;
+            const uint64_t vd = v_desc(v_tiles + vs * R::kBytes);
+            const uint32_t d = tmem + 256 + s * 128, pa = tmem + s * 128, desc = g.desc_pv;
 #pragma unroll
-            for (int i = 0; i < kTileKeys / 16; ++i)
-                mma_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, v_desc(va + i * 2048), g.desc_pv, j >= 2 || i > 0);
+            for (int i = 0; i < kTileKeys / 16; ++i) mma_ts(d, pa + i * 8, vd + i * (2048 >> 4), desc, j >= 2 || i > 0);
             umma_commit(&sh->pv_done[s]);
             if (!two || s) {
                 umma_commit(&sh->v_empty[vs]);
@@ -605,23 +612,34 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return *(float2 *)&r;
 }
 
+// Scores that the row does not see become minus infinity.  A pass of its own over the few tiles that need it: as a variant of
+// softmax_tile it doubled the unrolled code, whose instructions then came from beyond the nearest caches (12000 cycles a tile).
+__device__ __forceinline__ void mask_tile(uint32_t s_addr, const uint32_t (&seen)[4]) {
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+        const uint32_t bits = (c & 4 ? c & 2 ? seen[3] : seen[2] : c & 2 ? seen[1] : seen[0]) >> (c & 1) * 16;
+        if (__all_sync(0xffffffffu, (bits & 0xffffu) == 0xffffu)) continue;
+        float x[16];
+        uint32_t r[16];
+        tc::tmem_ld16(s_addr + c * 16, x);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i] = bits >> i & 1 ? __float_as_uint(x[i]) : 0xff800000u;
+        tmem_st16(s_addr + c * 16, r);
+    }
+    tmem_wait_st();
+}
+
 // One tile of a row: probabilities in place of the scores.  The maximum follows the tiles lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
 // saves nearly every pass over the accumulated output (a pass waits for the products of the tile before).
-template <int kDtype, int kHalves, bool kMasked>
+template <int kDtype, int kHalves>
 __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
-                                             uint64_t *pv_done, uint32_t pv_parity, const uint32_t (&seen)[4], Row &row) {
+                                             uint64_t *pv_done, uint32_t pv_parity, Row &row) {
     float x[128];
     tmem_ld128(s_addr, x);
     float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < 128; i += 2) {
-        if (kMasked) {
-            if (!(seen[i >> 5] >> (i & 31) & 1)) x[i] = -INFINITY;
-            if (!(seen[i >> 5] >> (i & 31) & 2)) x[i + 1] = -INFINITY;
-        }
-        top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
-    }
+    for (int i = 0; i < 128; i += 2) top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
     float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
     top = top == -INFINITY ? top : top * g.scale_log2;
     float shrink = 1.f;
@@ -656,10 +674,6 @@ __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint
             float2 y = fma2(make_float2(x[c * 32 + i], x[c * 32 + i + 1]), scale, minus);
             y.x = ex2_approx(y.x);
             y.y = ex2_approx(y.y);
-            if (kMasked) {               // (minus infinity times a scale of zero is not minus infinity)
-                if (!(seen[c] >> i & 1)) y.x = 0.f;
-                if (!(seen[c] >> i & 2)) y.y = 0.f;
-            }
             sum[i / 2 % 2] = add2(sum[i / 2 % 2], y);
             p[i / 2] = pack2<kDtype>(y.x, y.y);
         }
@@ -729,10 +743,8 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             tc_fence_after();
             if (active) {
                 const uint32_t o_addr = lanes + 256 + stream * 128, parity = (steps_done - 1) & 1;
-                const bool ok = masked ? softmax_tile<kDtype, kHalves, true>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
-                                                                             parity, seen, row)
-                                       : softmax_tile<kDtype, kHalves, false>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream],
-                                                                              parity, seen, row);
+                if (masked) mask_tile(s_addr, seen);
+                const bool ok = softmax_tile<kDtype, kHalves>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream], parity, row);
                 if (!ok) return false;
             }
             first = false;
@@ -774,20 +786,24 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = fmaf(o1[i], w[1], o[i]);
                 }
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    if (r >= u.rows || c * 32 + i >= a.D) continue;
+                if (r < u.rows) {
+                    const int cols = a.D - c * 32;
                     if (u.whole()) {
-                        uint4 y;
-                        y.x = pack2<kDtype>(o[i] * inv, o[i + 1] * inv);
-                        y.y = pack2<kDtype>(o[i + 2] * inv, o[i + 3] * inv);
-                        y.z = pack2<kDtype>(o[i + 4] * inv, o[i + 5] * inv);
-                        y.w = pack2<kDtype>(o[i + 6] * inv, o[i + 7] * inv);
-                        *(uint4 *)(out + c * 32 + i) = y;
+                        uint4 *to = (uint4 *)(out + c * 32);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 y;
+                            y.x = pack2<kDtype>(o[i] * inv, o[i + 1] * inv);
+                            y.y = pack2<kDtype>(o[i + 2] * inv, o[i + 3] * inv);
+                            y.z = pack2<kDtype>(o[i + 4] * inv, o[i + 5] * inv);
+                            y.w = pack2<kDtype>(o[i + 6] * inv, o[i + 7] * inv);
+                            if (i < cols) to[i / 8] = y;
+                        }
                     } else {
-                        float4 *y = (float4 *)(g.part_out + part * a.D + c * 32 + i);
-                        y[0] = make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
-                        y[1] = make_float4(o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv);
+                        float4 *to = (float4 *)(g.part_out + part * a.D + c * 32);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            if (i < cols) to[i / 4] = make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
                     }
                 }
                 if (bad && r < u.rows) add_not_finite<kDtype>(a, u, mask, c * 32, out, u.whole() ? nullptr : g.part_out + part * a.D);
@@ -883,12 +899,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 
 // ---- joining the parts of a unit -------------------------------------------------------------------------------------
 // A unit is split where the first tile of some CTA lies inside it.  Block c looks at the first tile of CTA c + 1 and joins the
-// unit that holds it, if that is the first such border in the unit; blockIdx.y takes kJoinRows of its rows, a warp per row.
-constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = 16;
+// unit that holds it, if that is the first such border in the unit; blockIdx.y takes kJoinRows of its rows, a warp per row.  The
+// parts' places are worked out by all threads together (64-bit divisions), a row's weights by its warp, and its
+// sums have the loads of eight parts in flight.
+constexpr int kJoinRows = 8;
+constexpr int kJoinThreads = 32 * kJoinRows;
+constexpr int kMaxCtas = 256;
 
 template <int kDtype>
 __global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid_constant__ AttnArgs g, int ctas) {
+    __shared__ int slot[kMaxCtas];                       // of the parts, in order of the keys
+    __shared__ float weight[kJoinRows][kMaxCtas];
+    __shared__ int parts;
     const spec_tree_attention_t &a = g.a;
     griddep_launch();
     griddep_wait();
@@ -899,46 +921,69 @@ __global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid
     const int b = find_tile(g, border, off);
     if (b >= a.B) return;
     const Seq s = seq_of(g, b, false);
-    const int unit = (int)(off / s.tiles), inside = (int)(off - (long long)unit * s.tiles);
+    const int unit = (int)((unsigned long long)off / (unsigned)s.tiles), inside = (int)(off - (long long)unit * s.tiles);
     const long long first = border - inside, last = first + s.tiles;
     if (inside == 0 || mine > first) return;
     const int blocks = s.units / a.Hkv, head = unit / blocks, row0 = (unit - head * blocks) * 2 * kTileRows;
-    const int rows = min(s.nodes * g.group - row0, 2 * kTileRows);
-    int parts = 1;                       // CTAs c .. c + parts - 1 hold parts; some may have no tile at all
-    while (c + parts < ctas && cta_start(tiles, c + parts, ctas) < last) ++parts;
-    for (int r = blockIdx.y * kJoinRows + warp; r < min(rows, ((int)blockIdx.y + 1) * kJoinRows); r += kJoinThreads / 32) {
-        const int col = lane * 4;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float top = -INFINITY, sum = 0.f;
-        for (int i = 0; i < parts; ++i) {
-            const long long begin = cta_start(tiles, c + i, ctas);
-            if (begin == cta_start(tiles, c + i + 1, ctas)) continue;
-            const size_t part = (size_t)(2 * (c + i) + (begin < first ? 1 : 0)) * g.part_rows + r;
-            const float lse = g.part_lse[part];
-            if (lse == -INFINITY) continue;
-            const float next = fmaxf(top, lse), keep = __expf(top - next), take = __expf(lse - next);
-            top = next;
-            sum = sum * keep + take;
-            if (col < a.D) {
-                const float4 o = *(const float4 *)(g.part_out + part * a.D + col);
-                // (a part whose weight is nothing still carries what is not finite)
-                acc.x = acc.x * keep + (fabsf(o.x) < INFINITY ? o.x * take : o.x);
-                acc.y = acc.y * keep + (fabsf(o.y) < INFINITY ? o.y * take : o.y);
-                acc.z = acc.z * keep + (fabsf(o.z) < INFINITY ? o.z * take : o.z);
-                acc.w = acc.w * keep + (fabsf(o.w) < INFINITY ? o.w * take : o.w);
-            }
+    const int rows = min(s.nodes * g.group - row0, 2 * kTileRows), r = blockIdx.y * kJoinRows + warp;
+    if (blockIdx.y * kJoinRows >= rows) return;
+    if (warp == 0) {                                     // CTAs c, c + 1, .. whose tiles begin before `last`; those without a tile have no part
+        int n = 0;
+        for (int i0 = c; i0 < ctas; i0 += 32) {
+            const int i = i0 + lane;
+            const long long begin = i < ctas ? cta_start(tiles, i, ctas) : last, end = i < ctas ? cta_start(tiles, i + 1, ctas) : last;
+            const bool has = begin < last && begin < end;
+            const unsigned all = __ballot_sync(0xffffffffu, has);
+            if (has) slot[n + __popc(all & ((1u << lane) - 1))] = 2 * i + (begin < first ? 1 : 0);
+            n += __popc(all);
+            if (__any_sync(0xffffffffu, begin >= last)) break;
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int node = (row0 + r) / g.group, h = head * g.group + row0 + r - node * g.group;
-        if (col < a.D) {
-            uint2 y;
-            y.x = pack2<kDtype>(acc.x * inv, acc.y * inv);
-            y.y = pack2<kDtype>(acc.z * inv, acc.w * inv);
-            *(uint2 *)((uint16_t *)a.out + b * a.out_stride[0] + node * a.out_stride[1] + h * a.out_stride[2] + col) = y;
-        }
-        if (lane == 0 && a.lse != nullptr)
-            a.lse[((size_t)b * a.T + node) * a.Hq + h] = sum == 0.f ? -INFINITY : top + logf(sum);
+        if (lane == 0) parts = n;
     }
+    __syncthreads();
+    if (r >= rows) return;
+    const int n = parts;
+    float top = -INFINITY, sum = 0.f;
+    for (int i = lane; i < n; i += 32) {
+        const float lse = g.part_lse[(size_t)slot[i] * g.part_rows + r];
+        weight[warp][i] = lse;
+        top = fmaxf(top, lse);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int i = lane; i < n; i += 32) {
+        const float lse = weight[warp][i], w = lse == -INFINITY ? 0.f : __expf(lse - top);
+        // (a part whose weight is nothing still carries what is not finite; one without a key carries nothing)
+        weight[warp][i] = lse == -INFINITY ? -1.f : w;
+        sum += w;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncwarp();
+    const int col = lane * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (col < a.D) {
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) {
+            const float4 o = *(const float4 *)(g.part_out + ((size_t)slot[i] * g.part_rows + r) * a.D + col);
+            const float w = weight[warp][i];
+            if (w < 0.f) continue;
+            acc.x += fabsf(o.x) < INFINITY ? o.x * w : o.x;
+            acc.y += fabsf(o.y) < INFINITY ? o.y * w : o.y;
+            acc.z += fabsf(o.z) < INFINITY ? o.z * w : o.z;
+            acc.w += fabsf(o.w) < INFINITY ? o.w * w : o.w;
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int node = (row0 + r) / g.group, h = head * g.group + row0 + r - node * g.group;
+    if (col < a.D) {
+        uint2 y;
+        y.x = pack2<kDtype>(acc.x * inv, acc.y * inv);
+        y.y = pack2<kDtype>(acc.z * inv, acc.w * inv);
+        *(uint2 *)((uint16_t *)a.out + b * a.out_stride[0] + node * a.out_stride[1] + h * a.out_stride[2] + col) = y;
+    }
+    if (lane == 0 && a.lse != nullptr)
+        a.lse[((size_t)b * a.T + node) * a.Hq + h] = sum == 0.f ? -INFINITY : top + logf(sum);
 }
 
 bool strides_ok(const int64_t (&s)[3]) { return s[0] >= 0 && s[1] >= 0 && s[2] >= 0 && !(s[0] % 8) && !(s[1] % 8) && !(s[2] % 8); }
@@ -984,7 +1029,7 @@ bool cache_map(const spec_tree_attention_t &a, const void *base, const int64_t (
 
 template <int kDtype, int kHalves>
 int launch(const AttnArgs &g, cudaStream_t st) {
-    const int ctas = num_sms();
+    const int ctas = num_sms() < kMaxCtas ? num_sms() : kMaxCtas;
     auto kernel = tree_attention_kernel<kDtype, kHalves>;
     SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<kHalves>()));
     SPEC_CUDA_TRY(launch_pdl(kernel, dim3(ctas), dim3(kThreads), smem_bytes<kHalves>(), st, g));
@@ -1025,7 +1070,8 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     AttnArgs g;
     g.a = *a;
     g.group = a->Hq / a->Hkv;
-    g.scale_log2 = fabsf(a->scale) * kLog2e;
+    // (not zero: what a row does not see is minus infinity times this)
+    g.scale_log2 = a->scale == 0.f ? 1e-30f : fabsf(a->scale) * kLog2e;
     const bool bf16 = a->dtype == SPEC_BF16;
     const uint32_t type = bf16 ? 1u << 7 | 1u << 10 : 0u;              // A and B: bf16 or fp16
     const uint32_t common = 1u << 4 | type | (uint32_t)(kTileRows >> 4) << 24;
