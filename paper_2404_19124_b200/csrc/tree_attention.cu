@@ -3,9 +3,9 @@
 //
 // Work.  A unit is a sequence, a key head and up to 256 of the query rows that share it (row = node * group + head within the
 // group); its keys, the cache's and then the tree's, are cut into tiles of 128.  All tiles of all units in a row are dealt to
-// the CTAs, one per SM, in equal runs, so that ragged batches and few long sequences fill the GPU alike.  A unit that a CTA
-// has to itself is written straight to `out`; of the others every CTA leaves its rows, normalised, with their log-sum-exp in
-// the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
+// the CTAs, one per SM, in runs of equal cost (a tile costs 2 for units of more than 128 rows, else 1), so that ragged batches and
+// few long sequences fill the GPU alike.  A unit that a CTA has to itself is written straight to `out`; of the others every CTA
+// leaves its rows, normalised, with their log-sum-exp in the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
 //
 // Roles of a CTA (16 warps):
 //   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
@@ -63,6 +63,21 @@ struct Ring {
 };
 constexpr int kMaxK = 6, kMaxV = 5;
 
+// The cost of the whole call is dealt to `ctas` CTAs: CTA c has the tiles that begin in [start(c), start(c + 1)).  None goes
+// without a tile, as tiles begin at most 2 (1 where no unit has more than 128 rows) apart.
+struct Deal {
+    long long cost;
+    int ctas;
+    __device__ long long start(int c) const {
+        return (unsigned long long)cost < 0x1000000ull ? (unsigned)cost * (unsigned)c / (unsigned)ctas
+                                                       : (unsigned long long)cost * (unsigned)c / (unsigned)ctas;
+    }
+    // whose is the tile that begins at `pos`
+    __device__ int owner(long long pos) const {
+        return (int)(((unsigned long long)(pos + 1) * (unsigned)ctas - 1) / (unsigned long long)cost);
+    }
+};
+
 struct Shared {
     uint64_t q_full[2], q_empty[2], k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
     uint64_t s_full[2], p_full[2], pv_done[2], meet, drained;
@@ -70,7 +85,8 @@ struct Shared {
     volatile int abort_flag;
     volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see load_v)
     int start_b;
-    long long start_off, pos, end;
+    long long start_off, left;
+    Deal deal;
     float stat[2][kTileRows][2];                // running maximum and sum of the two streams
 };
 template <int kHalves>
@@ -79,6 +95,7 @@ constexpr int smem_bytes() {
 }
 static_assert(smem_bytes<2>() <= 232448 && smem_bytes<1>() <= 232448, "shared memory of an SM");
 
+struct Join;
 struct AttnArgs {
     spec_tree_attention_t a;
     int group;                // query heads per key head
@@ -87,6 +104,8 @@ struct AttnArgs {
     float *part_out;          // [2 * CTAs][part_rows][D]
     float *part_lse;          // [2 * CTAs][part_rows]
     int part_rows;
+    Join *joins;              // [CTAs]
+    int max_len;              // of a sequence's cache
     int box_tokens;           // tokens of a TMA box, 0: the cache is not read by TMA (see cache_map)
     int box_pieces;           // kTileKeys / box_tokens
     CUtensorMap k_map, v_map; // the caches as (column, token, head, page)
@@ -114,69 +133,65 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Shared
 
 // ---- work ------------------------------------------------------------------------------------------------------------
 struct Seq {
-    int len, nodes, units, tiles;      // tiles: per unit
+    int len, nodes, row_tiles, tiles;  // row_tiles: of 128 rows, per key head; tiles: of 128 keys
+    __device__ long long head_cost() const { return (long long)row_tiles * tiles; }
 };
 
 __device__ __forceinline__ Seq seq_of(const AttnArgs &g, int b, bool report) {
     const spec_tree_attention_t &a = g.a;
-    const int cap = (int)min((long long)a.max_pages * a.page_size, (long long)INT_MAX - 4096);
     const int len = a.seq_len[b], nodes = a.n_nodes != nullptr ? a.n_nodes[b] : a.T;
     Seq s;
-    s.len = min(max(len, 0), cap);
+    s.len = min(max(len, 0), g.max_len);
     s.nodes = min(max(nodes, 0), a.T);
     if (report && (s.len != len || s.nodes != nodes)) report_error(a.err_word, SPEC_ERR_INDEX_RANGE);
-    s.units = a.Hkv * ((s.nodes * g.group + 2 * kTileRows - 1) / (2 * kTileRows));
+    s.row_tiles = (s.nodes * g.group + kTileRows - 1) / kTileRows;
     s.tiles = (s.len + s.nodes + kTileKeys - 1) / kTileKeys;
     return s;
 }
 
-__device__ __forceinline__ long long warp_inclusive_sum(long long x) {
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, off);
-        if ((threadIdx.x & 31) >= off) x += y;
-    }
-    return x;
-}
-
-// All tiles of the call; whole warp.
-__device__ long long all_tiles(const AttnArgs &g, bool report) {
-    long long sum = 0;
-    for (int b = threadIdx.x & 31; b < g.a.B; b += 32) {
+// Whole warp: the call's cost, and the sequence in which the part of CTA c begins with the offset in it (B: none).
+__device__ Deal deal_out(const AttnArgs &g, int c, bool report, int &b_out, long long &off_out) {
+    const int lane = threadIdx.x & 31;
+    long long cost = 0, mine = 0;
+    for (int b = lane; b < g.a.B; b += 32) {
         const Seq s = seq_of(g, b, report);
-        sum += (long long)s.units * s.tiles;
+        mine = g.a.Hkv * s.head_cost();
+        cost += mine;
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    return sum;
-}
-
-// The sequence that tile `pos` belongs to and the tile's place in it; whole warp.  B if there is none.
-__device__ int find_tile(const AttnArgs &g, long long pos, long long &off) {
+    for (int off = 16; off > 0; off >>= 1) cost += __shfl_xor_sync(0xffffffffu, cost, off);
+    Deal d;
+    d.cost = cost;
+    const long long most = g.a.T * g.group > kTileRows ? (cost > 2 ? cost / 2 : cost ? 1 : 0) : cost;
+    d.ctas = (int)min((long long)gridDim.x, most);
+    b_out = g.a.B;
+    off_out = 0;
+    if (c >= d.ctas) return d;
+    const long long pos = d.start(c);
     long long before = 0;
     for (int b0 = 0; b0 < g.a.B; b0 += 32) {
-        const int b = b0 + (threadIdx.x & 31);
-        long long mine = 0;
-        if (b < g.a.B) {
-            const Seq s = seq_of(g, b, false);
-            mine = (long long)s.units * s.tiles;
+        const int b = b0 + lane;
+        if (g.a.B > 32 || b >= g.a.B) {
+            mine = 0;
+            if (b < g.a.B) mine = g.a.Hkv * seq_of(g, b, false).head_cost();
         }
-        const long long upto = before + warp_inclusive_sum(mine);
+        long long upto = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += y;
+        }
+        upto += before;
         const unsigned hit = __ballot_sync(0xffffffffu, upto > pos);
         if (hit) {
-            const int lane = __ffs(hit) - 1;
-            off = pos - __shfl_sync(0xffffffffu, upto - mine, lane);
-            return b0 + lane;
+            const int who = __ffs(hit) - 1;
+            off_out = pos - __shfl_sync(0xffffffffu, upto - mine, who);
+            b_out = b0 + who;
+            return d;
         }
         before = __shfl_sync(0xffffffffu, upto, 31);
     }
-    off = 0;
-    return g.a.B;
-}
-
-__device__ __forceinline__ long long cta_start(long long tiles, int cta, int ctas) {
-    return (unsigned long long)tiles < 0x1000000ull ? (unsigned)tiles * (unsigned)cta / (unsigned)ctas
-                                                     : (unsigned long long)tiles * (unsigned)cta / (unsigned)ctas;
+    return d;
 }
 
 // A unit's tiles [t0, t1) that this CTA has.
@@ -184,55 +199,71 @@ struct Unit {
     int b, head, row0, rows;           // rows row0 .. row0 + rows - 1 of the head's nodes * group
     int len, nodes, tiles, t0, t1;
     int index;                         // counts the CTA's units
+    long long begin;                   // in the cost of the call
     __device__ bool two_tiles() const { return rows > kTileRows; }
     __device__ bool whole() const { return t0 == 0 && t1 == tiles; }
 };
 
 struct Walk {
     Seq s;
-    int b, unit, tile, index;
-    long long pos, end;
+    int b, head, row_tile, index;      // row_tile: the unit's first
+    int off;                           // cost of the unit that is behind
+    long long left, end;               // cost of this CTA that is ahead; where it ends
     __device__ Walk(const AttnArgs &g, const Shared *sh) {
         b = sh->start_b;
-        pos = sh->pos;
-        end = sh->end;
-        index = 0;
-        unit = tile = 0;
+        left = sh->left;
+        end = 0;
+        index = head = row_tile = off = 0;
         s = {0, 0, 0, 0};
         if (b < g.a.B) {
             s = seq_of(g, b, false);
-            unit = (int)(sh->start_off / s.tiles);
-            tile = (int)(sh->start_off - (long long)unit * s.tiles);
+            head = (int)(sh->start_off / s.head_cost());
+            const long long in_head = sh->start_off - head * s.head_cost();
+            row_tile = (int)(in_head / (2 * s.tiles)) * 2;
+            off = (int)(in_head - (long long)row_tile * s.tiles);
+            end = sh->deal.start(blockIdx.x + 1);
         }
     }
     __device__ bool next(const AttnArgs &g, Unit &u) {
-        while (pos < end && b < g.a.B) {
-            if (unit >= s.units) {
-                unit = tile = 0;
+        while (left > 0 && b < g.a.B) {
+            if (row_tile >= s.row_tiles) {
+                row_tile = 0;
+                ++head;
+            }
+            if (head >= g.a.Hkv || s.row_tiles == 0) {
+                head = 0;
                 if (++b < g.a.B) s = seq_of(g, b, false);
                 continue;
             }
-            const int blocks = s.units / g.a.Hkv, head = unit / blocks;
+            const int two = row_tile + 1 < s.row_tiles ? 1 : 0, cost = s.tiles << two;
+            const int take = (int)min((long long)(cost - off), left);
             u.b = b;
             u.head = head;
-            u.row0 = (unit - head * blocks) * 2 * kTileRows;
+            u.row0 = row_tile * kTileRows;
             u.rows = min(s.nodes * g.group - u.row0, 2 * kTileRows);
             u.len = s.len;
             u.nodes = s.nodes;
             u.tiles = s.tiles;
-            u.t0 = tile;
-            u.t1 = (int)min((long long)s.tiles, tile + (end - pos));
-            u.index = index++;
-            pos += u.t1 - u.t0;
-            tile = u.t1;
-            if (tile == s.tiles) {
-                ++unit;
-                tile = 0;
+            u.t0 = (off + two) >> two;
+            u.t1 = (off + take + two) >> two;
+            u.begin = end - left - off;
+            left -= take;
+            off += take;
+            if (off == cost) {
+                row_tile += 2;
+                off = 0;
             }
+            if (u.t0 == u.t1) continue;                  // the second half of a tile that begins in the CTA before
+            u.index = index++;
             return true;
         }
         return false;
     }
+};
+
+// What block c of tree_combine_kernel joins: the unit whose first tiles, but not all, CTA c has.  rows 0: nothing.
+struct __align__(16) Join {
+    int b, head, row0, rows, parts, slot, pad[2];       // slot: of the first part; part i > 0 is in slot 2 (c + i)
 };
 
 // ---- loads -----------------------------------------------------------------------------------------------------------
@@ -815,7 +846,13 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             }
         }
         if (!softmax_meet(sh, meet, a.err_word)) return false;       // nobody writes O, stat or the flag while somebody may still read them
-        if (threadIdx.x == 0) sh->not_finite[u.index % kUnitFlags] = 0;
+        if (threadIdx.x == 0) {
+            sh->not_finite[u.index % kUnitFlags] = 0;
+            if (u.t0 == 0 && !u.whole())
+                g.joins[blockIdx.x] = {u.b, u.head, u.row0, u.rows,
+                                       sh->deal.owner(u.begin + ((long long)(u.tiles - 1) << (two ? 1 : 0))) - (int)blockIdx.x + 1,
+                                       2 * (int)blockIdx.x + (u.index ? 1 : 0), {}};
+        }
     }
     return true;
 }
@@ -858,15 +895,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     }
     griddep_wait();
     if (warp == 1) {
-        const long long tiles = all_tiles(g, blockIdx.x == 0);
-        const long long pos = cta_start(tiles, blockIdx.x, gridDim.x), end = cta_start(tiles, blockIdx.x + 1, gridDim.x);
-        long long off = 0;
-        const int b = pos < end ? find_tile(g, pos, off) : g.a.B;
+        int b;
+        long long off;
+        const Deal d = deal_out(g, blockIdx.x, blockIdx.x == 0, b, off);
         if ((threadIdx.x & 31) == 0) {
             sh->start_b = b;
             sh->start_off = off;
-            sh->pos = pos;
-            sh->end = end;
+            sh->left = (int)blockIdx.x < d.ctas ? d.start(blockIdx.x + 1) - d.start(blockIdx.x) : 0;
+            sh->deal = d;
+            g.joins[blockIdx.x] = Join{};                // (softmax_role writes what there is to join)
         }
     }
     tc_fence_before();
@@ -898,54 +935,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 }
 
 // ---- joining the parts of a unit -------------------------------------------------------------------------------------
-// A unit is split where the first tile of some CTA lies inside it.  Block c looks at the first tile of CTA c + 1 and joins the
-// unit that holds it, if that is the first such border in the unit; blockIdx.y takes kJoinRows of its rows, a warp per row.  The
-// parts' places are worked out by all threads together (64-bit divisions), a row's weights by its warp, and its
-// sums have the loads of eight parts in flight.
+// Block c joins the unit that CTA c began and others ended, if there is one: CTA c left it in joins[c].  blockIdx.y takes
+// kJoinRows of its rows, a warp per row; a row's weights are worked out by its warp, and its sums have the loads of eight parts in
+// flight.
 constexpr int kJoinRows = 8;
 constexpr int kJoinThreads = 32 * kJoinRows;
 constexpr int kMaxCtas = 256;
 
 template <int kDtype>
-__global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid_constant__ AttnArgs g, int ctas) {
-    __shared__ int slot[kMaxCtas];                       // of the parts, in order of the keys
+__global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid_constant__ AttnArgs g) {
     __shared__ float weight[kJoinRows][kMaxCtas];
-    __shared__ int parts;
     const spec_tree_attention_t &a = g.a;
     griddep_launch();
     griddep_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x;
-    const long long tiles = all_tiles(g, false), border = cta_start(tiles, c + 1, ctas), mine = cta_start(tiles, c, ctas);
-    if (mine == border || border >= tiles) return;
-    long long off;
-    const int b = find_tile(g, border, off);
-    if (b >= a.B) return;
-    const Seq s = seq_of(g, b, false);
-    const int unit = (int)((unsigned long long)off / (unsigned)s.tiles), inside = (int)(off - (long long)unit * s.tiles);
-    const long long first = border - inside, last = first + s.tiles;
-    if (inside == 0 || mine > first) return;
-    const int blocks = s.units / a.Hkv, head = unit / blocks, row0 = (unit - head * blocks) * 2 * kTileRows;
-    const int rows = min(s.nodes * g.group - row0, 2 * kTileRows), r = blockIdx.y * kJoinRows + warp;
-    if (blockIdx.y * kJoinRows >= rows) return;
-    if (warp == 0) {                                     // CTAs c, c + 1, .. whose tiles begin before `last`; those without a tile have no part
-        int n = 0;
-        for (int i0 = c; i0 < ctas; i0 += 32) {
-            const int i = i0 + lane;
-            const long long begin = i < ctas ? cta_start(tiles, i, ctas) : last, end = i < ctas ? cta_start(tiles, i + 1, ctas) : last;
-            const bool has = begin < last && begin < end;
-            const unsigned all = __ballot_sync(0xffffffffu, has);
-            if (has) slot[n + __popc(all & ((1u << lane) - 1))] = 2 * i + (begin < first ? 1 : 0);
-            n += __popc(all);
-            if (__any_sync(0xffffffffu, begin >= last)) break;
-        }
-        if (lane == 0) parts = n;
-    }
-    __syncthreads();
-    if (r >= rows) return;
-    const int n = parts;
+    const Join j = g.joins[c];
+    const int b = j.b, head = j.head, row0 = j.row0, n = j.parts, r = blockIdx.y * kJoinRows + warp;
+    if (r >= j.rows) return;
+    // part i's rows
+    auto place = [&](int i) { return (size_t)(i ? 2 * (c + i) : j.slot) * g.part_rows + r; };
     float top = -INFINITY, sum = 0.f;
     for (int i = lane; i < n; i += 32) {
-        const float lse = g.part_lse[(size_t)slot[i] * g.part_rows + r];
+        const float lse = g.part_lse[place(i)];
         weight[warp][i] = lse;
         top = fmaxf(top, lse);
     }
@@ -965,7 +976,7 @@ __global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const __grid
     if (col < a.D) {
 #pragma unroll 8
         for (int i = 0; i < n; ++i) {
-            const float4 o = *(const float4 *)(g.part_out + ((size_t)slot[i] * g.part_rows + r) * a.D + col);
+            const float4 o = *(const float4 *)(g.part_out + place(i) * a.D + col);
             const float w = weight[warp][i];
             if (w < 0.f) continue;
             acc.x += fabsf(o.x) < INFINITY ? o.x * w : o.x;
@@ -998,9 +1009,9 @@ int part_rows(int T, int Hq, int Hkv) {
     const long long rows = (long long)T * (Hq / Hkv);
     return rows < 2 * kTileRows ? (int)rows : 2 * kTileRows;
 }
-size_t part_lse_bytes(int T, int Hq, int Hkv) {
-    return ((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * 4 + kWsAlign - 1) / kWsAlign * kWsAlign;
-}
+size_t aligned(size_t bytes) { return (bytes + kWsAlign - 1) / kWsAlign * kWsAlign; }
+size_t part_lse_bytes(int T, int Hq, int Hkv) { return aligned((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * 4); }
+size_t join_bytes() { return aligned((size_t)num_sms() * sizeof(Join)); }
 
 // The cache as a TMA tensor whose boxes are a page, or 128 tokens of one, by 64 columns of a head.  Pages have to tile 128 keys
 // or be tiled by them, in whole groups of 8 rows (the swizzle's period).  False: not such a cache, or strides that TMA does not take.
@@ -1033,8 +1044,8 @@ int launch(const AttnArgs &g, cudaStream_t st) {
     auto kernel = tree_attention_kernel<kDtype, kHalves>;
     SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<kHalves>()));
     SPEC_CUDA_TRY(launch_pdl(kernel, dim3(ctas), dim3(kThreads), smem_bytes<kHalves>(), st, g));
-    SPEC_CUDA_TRY(launch_pdl(tree_combine_kernel<kDtype>, dim3(ctas - 1, (g.part_rows + kJoinRows - 1) / kJoinRows),
-                             dim3(kJoinThreads), 0, st, g, ctas));
+    SPEC_CUDA_TRY(launch_pdl(tree_combine_kernel<kDtype>, dim3(ctas, (g.part_rows + kJoinRows - 1) / kJoinRows),
+                             dim3(kJoinThreads), 0, st, g));
     return SPEC_OK;
 }
 
@@ -1047,7 +1058,7 @@ extern "C" {
 
 size_t spec_tree_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
     if (check_shape(B, T, Hq, Hkv, D) != SPEC_OK) return 0;
-    return part_lse_bytes(T, Hq, Hkv) + ((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * D * 4 + kWsAlign - 1) / kWsAlign * kWsAlign;
+    return join_bytes() + part_lse_bytes(T, Hq, Hkv) + aligned((size_t)2 * num_sms() * part_rows(T, Hq, Hkv) * D * 4);
 }
 
 int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t workspace_bytes, void *cuda_stream) {
@@ -1078,8 +1089,11 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     g.desc_qk = common | (uint32_t)(kTileKeys >> 3) << 17 | (a->scale < 0.f ? 1u << 13 : 0u);       // a negative scale negates Q
     g.desc_pv = common | (uint32_t)((a->D + 15) / 16 * 2) << 17 | 1u << 16;                         // V is MN-major
     g.part_rows = part_rows(a->T, a->Hq, a->Hkv);
-    g.part_lse = (float *)workspace;
-    g.part_out = (float *)((char *)workspace + part_lse_bytes(a->T, a->Hq, a->Hkv));
+    g.joins = (Join *)workspace;
+    g.part_lse = (float *)((char *)workspace + join_bytes());
+    g.part_out = (float *)((char *)g.part_lse + part_lse_bytes(a->T, a->Hq, a->Hkv));
+    const long long most = (long long)a->max_pages * a->page_size;
+    g.max_len = (int)(most < INT_MAX - 4096 ? most : INT_MAX - 4096);
     g.box_tokens = a->page_size % 8 ? 0 : kTileKeys % a->page_size == 0 ? a->page_size : a->page_size % kTileKeys == 0 ? kTileKeys : 0;
     if (g.box_tokens && (!cache_map(*a, a->k_cache, a->kc_stride, g.box_tokens, &g.k_map) ||
                          !cache_map(*a, a->v_cache, a->vc_stride, g.box_tokens, &g.v_map)))
