@@ -3,7 +3,7 @@
 //
 // Work.  A unit is a sequence, a key head and up to 256 of the query rows that share it (row = node * group + head within the
 // group); its keys, the cache's and then the tree's, are cut into tiles of 128.  All tiles of all units in a row are dealt to
-// the CTAs, one per SM, in runs of equal cost (a tile costs 2 for units of more than 128 rows, else 1), so that ragged batches and
+// the CTAs, one per SM, in runs of equal cost (a tile costs 2 for units of more than 128 rows, else 1; see Deal), so that ragged batches and
 // few long sequences fill the GPU alike.  A unit that a CTA has to itself is written straight to `out`; of the others every CTA
 // leaves its rows, normalised, with their log-sum-exp in the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
 //
@@ -11,10 +11,10 @@
 //   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
 //                   TMEM in place of the scores, results
 //   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 128], O += P V, P read from TMEM
-//   warps 9-11      nothing (registers are given away by groups of four warps)
-//   warps 12-15     load tiles of Q, K and V, 128-byte-swizzled: tiles that lie in the cache as TMA boxes, a page (or 128 tokens of
-//                   one) by 64 columns each; the tile in which the cache ends and the tree begins, the tree, Q, and caches whose
-//                   pages do not tile 128 keys row by row with 16-byte asynchronous copies (rows that do not exist read as zeros)
+//   warps 9-11      bring the tiles of K and V that lie in the cache, as TMA boxes: a page (or 128 tokens of one) by 64 columns
+//   warps 12-15     bring the others row by row with 16-byte asynchronous copies (rows that do not exist read as zeros): Q, the tile
+//                   in which the cache ends and the tree begins, the tree, and caches whose pages do not tile 128 keys
+// Tiles are 128-byte-swizzled either way.
 // Two streams keep the tensor cores busy while a softmax runs.  Units of more than 128 rows have a stream per 128 rows, both on the
 // same tile of keys; smaller ones give their tiles to the streams in turn, and the two results are joined at the end.
 #include <limits.h>
@@ -43,14 +43,18 @@ constexpr int kTileKeys = 128;
 constexpr int kTileRows = 128;
 constexpr int kHalfBytes = kTileKeys * 128;     // 64 columns of a tile of 128 rows
 constexpr int kSoftmaxThreads = 256;
+constexpr int kBoxWarps = 3;
 constexpr int kLoadThreads = 128;
-constexpr int kFirstLoader = kSoftmaxThreads + 128;
+constexpr int kFirstLoader = kSoftmaxThreads + 32 * (1 + kBoxWarps);
 constexpr int kThreads = kFirstLoader + kLoadThreads;
-// Registers of a thread after the roles have parted; 2 * 128 * (192 + 64) is what the launch has (512 threads of 128).  (All that the
+// A tile of K or V is complete after kBoxWarps arrivals of kLoadThreads each (TMA) or kLoadThreads of kBoxWarps each (copies).
+constexpr int kTileArrivals = kBoxWarps * kLoadThreads;
+// Registers of a thread after the roles have parted; 2 * 128 * (184 + 72) is what the launch has (512 threads of 128).  (All that the
 // roles call is inlined: around a call the compiler does not go beyond the launch's 128.)
 constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
 constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns each
 constexpr int kUnitFlags = 8;
+constexpr uint32_t kSpinMax = 1u << 22;         // polls of a wait, 64 ns and more each, before it gives up
 constexpr float kRescaleAbove = 8.f;            // see softmax_tile
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -63,11 +67,14 @@ struct Ring {
 };
 constexpr int kMaxK = 6, kMaxV = 5;
 
-// The cost of the whole call is dealt to `ctas` CTAs: CTA c has the tiles that begin in [start(c), start(c + 1)).  None goes
-// without a tile, as tiles begin at most 2 (1 where no unit has more than 128 rows) apart.
+// The cost of the whole call is dealt to `ctas` CTAs: CTA c has the tiles that begin in [start(c), start(c + 1)).  A unit costs
+// unit_cost beside its tiles, behind its first one: what its end takes (a masked tile, results, a pipeline that empties) is time that
+// no tile explains.  CTAs are as few as it takes for each to have a tile in every unit that its run meets.
+constexpr int kUnitCost = 3;           // where CTAs have at least kManyTiles of cost each, else 0
+constexpr int kManyTiles = 16;
 struct Deal {
     long long cost;
-    int ctas;
+    int ctas, unit_cost;
     __device__ long long start(int c) const {
         return (unsigned long long)cost < 0x1000000ull ? (unsigned)cost * (unsigned)c / (unsigned)ctas
                                                        : (unsigned long long)cost * (unsigned)c / (unsigned)ctas;
@@ -80,7 +87,7 @@ struct Deal {
 
 struct Shared {
     uint64_t q_full[2], q_empty[2], k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
-    uint64_t s_full[2], p_full[2], pv_done[2], meet, drained;
+    uint64_t s_full[2], p_full[2], pv_done[2], meet, drained, boxes_asked, rows_asked;
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see load_v)
@@ -112,7 +119,7 @@ struct AttnArgs {
 };
 
 __device__ __forceinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
-    for (uint32_t it = 0; it < tc::kSpinMax; ++it) {
+    for (uint32_t it = 0; it < kSpinMax; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
         if (it > tc::kSpinFast) {
             if (sh->abort_flag) return false;
@@ -134,7 +141,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Shared
 // ---- work ------------------------------------------------------------------------------------------------------------
 struct Seq {
     int len, nodes, row_tiles, tiles;  // row_tiles: of 128 rows, per key head; tiles: of 128 keys
-    __device__ long long head_cost() const { return (long long)row_tiles * tiles; }
+    __device__ long long head_cost(int unit_cost) const { return (long long)row_tiles * tiles + (row_tiles + 1) / 2 * unit_cost; }
 };
 
 __device__ __forceinline__ Seq seq_of(const AttnArgs &g, int b, bool report) {
@@ -152,18 +159,22 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs &g, int b, bool report) {
 // Whole warp: the call's cost, and the sequence in which the part of CTA c begins with the offset in it (B: none).
 __device__ Deal deal_out(const AttnArgs &g, int c, bool report, int &b_out, long long &off_out) {
     const int lane = threadIdx.x & 31;
-    long long cost = 0, mine = 0;
+    long long cost = 0, units = 0, mine = 0;
     for (int b = lane; b < g.a.B; b += 32) {
         const Seq s = seq_of(g, b, report);
-        mine = g.a.Hkv * s.head_cost();
-        cost += mine;
+        cost += g.a.Hkv * s.head_cost(0);
+        if (s.tiles) units += g.a.Hkv * ((s.row_tiles + 1) / 2);
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) cost += __shfl_xor_sync(0xffffffffu, cost, off);
+    for (int off = 16; off > 0; off >>= 1) {
+        cost += __shfl_xor_sync(0xffffffffu, cost, off);
+        units += __shfl_xor_sync(0xffffffffu, units, off);
+    }
     Deal d;
-    d.cost = cost;
-    const long long most = g.a.T * g.group > kTileRows ? (cost > 2 ? cost / 2 : cost ? 1 : 0) : cost;
-    d.ctas = (int)min((long long)gridDim.x, most);
+    d.unit_cost = cost >= (long long)kManyTiles * gridDim.x ? kUnitCost : 0;
+    d.cost = cost = cost + units * d.unit_cost;
+    const int apart = d.unit_cost + (g.a.T * g.group > kTileRows ? 2 : 1);       // the most between the begins of two tiles
+    d.ctas = (int)min((long long)gridDim.x, cost > apart ? cost / apart : cost ? 1 : 0);
     b_out = g.a.B;
     off_out = 0;
     if (c >= d.ctas) return d;
@@ -171,10 +182,7 @@ __device__ Deal deal_out(const AttnArgs &g, int c, bool report, int &b_out, long
     long long before = 0;
     for (int b0 = 0; b0 < g.a.B; b0 += 32) {
         const int b = b0 + lane;
-        if (g.a.B > 32 || b >= g.a.B) {
-            mine = 0;
-            if (b < g.a.B) mine = g.a.Hkv * seq_of(g, b, false).head_cost();
-        }
+        mine = b < g.a.B ? g.a.Hkv * seq_of(g, b, false).head_cost(d.unit_cost) : 0;
         long long upto = mine;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
@@ -207,22 +215,29 @@ struct Unit {
 struct Walk {
     Seq s;
     int b, head, row_tile, index;      // row_tile: the unit's first
-    int off;                           // cost of the unit that is behind
+    int off, unit_cost;                // cost of the unit that is behind
     long long left, end;               // cost of this CTA that is ahead; where it ends
     __device__ Walk(const AttnArgs &g, const Shared *sh) {
         b = sh->start_b;
         left = sh->left;
         end = 0;
-        index = head = row_tile = off = 0;
+        index = head = row_tile = off = unit_cost = 0;
         s = {0, 0, 0, 0};
         if (b < g.a.B) {
+            unit_cost = sh->deal.unit_cost;
             s = seq_of(g, b, false);
-            head = (int)(sh->start_off / s.head_cost());
-            const long long in_head = sh->start_off - head * s.head_cost();
-            row_tile = (int)(in_head / (2 * s.tiles)) * 2;
-            off = (int)(in_head - (long long)row_tile * s.tiles);
+            const long long head_cost = s.head_cost(unit_cost);
+            head = (int)(sh->start_off / head_cost);
+            const long long in_head = sh->start_off - head * head_cost;
+            const int pair_cost = 2 * s.tiles + unit_cost;               // of every unit of a head but the last
+            row_tile = (int)(in_head / pair_cost) * 2;
+            off = (int)(in_head - (long long)(row_tile / 2) * pair_cost);
             end = sh->deal.start(blockIdx.x + 1);
         }
+    }
+    // the tiles of a unit that begin before `upto` in it
+    __device__ int tiles_before(int upto, int two) const {
+        return upto <= 0 ? 0 : max(1, (upto - unit_cost + two) >> two);
     }
     __device__ bool next(const AttnArgs &g, Unit &u) {
         while (left > 0 && b < g.a.B) {
@@ -235,7 +250,7 @@ struct Walk {
                 if (++b < g.a.B) s = seq_of(g, b, false);
                 continue;
             }
-            const int two = row_tile + 1 < s.row_tiles ? 1 : 0, cost = s.tiles << two;
+            const int two = row_tile + 1 < s.row_tiles ? 1 : 0, cost = (s.tiles << two) + unit_cost;
             const int take = (int)min((long long)(cost - off), left);
             u.b = b;
             u.head = head;
@@ -244,8 +259,8 @@ struct Walk {
             u.len = s.len;
             u.nodes = s.nodes;
             u.tiles = s.tiles;
-            u.t0 = (off + two) >> two;
-            u.t1 = (off + take + two) >> two;
+            u.t0 = tiles_before(off, two);
+            u.t1 = tiles_before(off + take, two);
             u.begin = end - left - off;
             left -= take;
             off += take;
@@ -253,7 +268,7 @@ struct Walk {
                 row_tile += 2;
                 off = 0;
             }
-            if (u.t0 == u.t1) continue;                  // the second half of a tile that begins in the CTA before
+            if (u.t0 == u.t1) continue;                  // what is left of a tile that begins in the CTA before
             u.index = index++;
             return true;
         }
@@ -328,14 +343,22 @@ __device__ __forceinline__ const uint16_t *row_of(KeyPlace p, int b, int head, c
     return nullptr;
 }
 
-// The boxes of a whole tile of the cache are dealt to the four loading warps: box i is piece i / kHalves of 128 / box_tokens,
-// columns 64 * (i % kHalves).  Lane l of a warp looks up the page of the warp's box l, a tile ahead.  Nothing here divides but where
-// a page holds several tiles: with a division per box and lookups that the copies wait for, four warps brought in 2.8 TB/s.
-constexpr int kMaxBoxes = 8;                             // of a warp: pages of 8 tokens, two halves
+__device__ __forceinline__ void mbar_arrive_n(uint64_t *bar, int n) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
+// Tiles [t0, boxed) of a unit lie in the cache and come by TMA.
+__device__ __forceinline__ int boxed_tiles(const AttnArgs &g, const Unit &u) {
+    return g.box_tokens ? min(u.t1, max(u.t0, u.len / kTileKeys)) : u.t0;
+}
+
+// The boxes of a tile are dealt to the warps: box i is piece i / kHalves of 128 / box_tokens, columns 64 * (i % kHalves).  Lane l
+// of a warp looks up the page of the warp's box l, a tile ahead.  Nothing here divides but where a page holds several tiles:
+// with a division per box and lookups that the copies wait for, four warps brought in 2.8 TB/s.
+constexpr int kMaxBoxes = (32 + kBoxWarps - 1) / kBoxWarps;              // of a warp: pages of 8 tokens, two halves
 template <int kHalves>
 __device__ __forceinline__ int box_page(const AttnArgs &g, const Unit &u, int tile, int warp, int lane) {
     const spec_tree_attention_t &a = g.a;
-    const int piece = (warp + 4 * lane) / kHalves;
+    const int piece = (warp + kBoxWarps * lane) / kHalves;
     if (piece >= g.box_pieces) return 0;
     const int index = a.page_size > kTileKeys ? tile / (a.page_size / kTileKeys) : tile * g.box_pieces + piece;
     const int id = a.block_table[u.b * a.table_stride + index];
@@ -352,45 +375,113 @@ __device__ __forceinline__ void load_boxes(const AttnArgs &g, const CUtensorMap 
 #pragma unroll
     for (int i = 0; i < kMaxBoxes; ++i) id[i] = __shfl_sync(0xffffffffu, page, i);
     if (tc::elect_one()) {
-        if (warp < boxes) tc::mbar_arrive_expect_tx(bar, (boxes - warp + 3) / 4 * bytes);
-        else mbar_arrive(bar);
+        int arrivals = kLoadThreads;
+        if (warp < boxes) {
+            tc::mbar_arrive_expect_tx(bar, (boxes - warp + kBoxWarps - 1) / kBoxWarps * bytes);
+            --arrivals;
+        }
+        mbar_arrive_n(bar, arrivals);
 #pragma unroll
         for (int i = 0; i < kMaxBoxes; ++i) {
-            const int box = warp + 4 * i, piece = box / kHalves, half = box % kHalves;
+            const int box = warp + kBoxWarps * i, piece = box / kHalves, half = box % kHalves;
             if (box >= boxes) break;
             asm volatile(
                 "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                 ::"r"(dst + half * kHalfBytes + piece * bytes), "l"((uint64_t)map), "r"(half * 64), "r"(token), "r"(u.head),
                 "r"(id[i]), "r"(smem_u32(bar)) : "memory");
         }
-    } else {
-        mbar_arrive(bar);
     }
     __syncwarp();
 }
 
-// Is one of the eight numbers not finite?  (bf16 has eight exponent bits, fp16 five.)
-template <int kDtype>
-__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x, bool &bad) {
-    constexpr uint32_t kExp = kDtype == SPEC_BF16 ? 0x7f80u : 0x7c00u;
-    if ((x & kExp) == kExp) {
-        bad = true;
-        x &= 0xffff0000u;
+// K of a tile goes ahead of V of the tile before.  Every tile of a unit takes the next slot, whoever fills it, so a role passes over
+// the slots that the other one fills.  A barrier's parity tells its phases apart only for those that are at most one phase away
+// from it: row_role turns to the last tiles of a unit when box_role has asked for those before them (boxes_asked), and box_role to
+// the next unit when row_role has a slot for each of the last ones (rows_asked).
+template <int kSlots>
+__device__ __forceinline__ void pass_over(int n, int &slot, uint32_t &parity) {
+    slot += n;
+    parity ^= (slot / kSlots) & 1;
+    slot %= kSlots;
+}
+
+template <int kHalves>
+__device__ void box_role(const AttnArgs &g, Shared *sh, uint32_t k_tiles, uint32_t v_tiles) {
+    using R = Ring<kHalves>;
+    const int warp = (threadIdx.x >> 5) - (kSoftmaxThreads / 32 + 1), lane = threadIdx.x & 31;
+    int ks = 0, vs = 0;                                  // slots, and the parity of their `empty` that means free
+    uint32_t kp = 1, vp = 1, rows_parity = 0;
+    Walk walk(g, sh);
+    Unit u;
+    while (walk.next(g, u)) {
+        const int boxed = boxed_tiles(g, u);
+        int page = u.t0 < boxed ? box_page<kHalves>(g, u, u.t0, warp, lane) : 0, before = 0;
+        for (int t = u.t0; t <= boxed; ++t) {
+            const int now = page;
+            if (t < boxed) {
+                if (t + 1 < boxed) page = box_page<kHalves>(g, u, t + 1, warp, lane);   // (ahead of the wait)
+                if (!warp_wait(&sh->k_empty[ks], kp, sh, g.a.err_word)) return;
+                load_boxes<kHalves>(g, &g.k_map, u, t, now, warp, k_tiles + ks * R::kBytes, &sh->k_full[ks]);
+                pass_over<R::kK>(1, ks, kp);
+            } else if (boxed < u.t1 && lane == 0) {
+                mbar_arrive(&sh->boxes_asked);
+            }
+            if (t > u.t0) {
+                if (!warp_wait(&sh->v_empty[vs], vp, sh, g.a.err_word)) return;
+                load_boxes<kHalves>(g, &g.v_map, u, t - 1, before, warp, v_tiles + vs * R::kBytes, &sh->v_full[vs]);
+                pass_over<R::kV>(1, vs, vp);
+            }
+            before = now;
+        }
+        if (boxed < u.t1) {
+            if (!warp_wait(&sh->rows_asked, rows_parity, sh, g.a.err_word)) return;
+            rows_parity ^= 1;
+            pass_over<R::kK>(u.t1 - boxed, ks, kp);
+            pass_over<R::kV>(u.t1 - boxed, vs, vp);
+        }
     }
-    if ((x >> 16 & kExp) == kExp) {
-        bad = true;
-        x &= 0x0000ffffu;
+}
+
+// Rows of the tree in a tile of V.  Not every query sees them, and 0 * inf would reach those that do not: what is not finite becomes zero
+// in the tile, and the rows that do see it take it from memory (add_not_finite).  Every thread looks at the chunks that it
+// copied itself, after they have arrived and before it says so.
+template <int kDtype, int kHalves>
+__device__ __forceinline__ bool finite_values(const TileMap<kHalves> &map, uint32_t tile, int first, int end, int cols) {
+    constexpr uint32_t kExp = kDtype == SPEC_BF16 ? 0x7f80u : 0x7c00u;       // eight or five exponent bits
+    bool bad = false;
+    if (map.chunk * 8 < cols) {
+#pragma unroll 4
+        for (int i = 0; i < TileMap<kHalves>::kPasses; ++i) {
+            const int r = map.row + i * TileMap<kHalves>::kStep;
+            const uint32_t at = map.address(tile, r);
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+            bool found = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) found |= (x[e] & kExp) == kExp || (x[e] >> 16 & kExp) == kExp;
+            if (found && r >= first && r < end) {
+                bad = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] &= ((x[e] & kExp) == kExp ? 0u : 0x0000ffffu) | ((x[e] >> 16 & kExp) == kExp ? 0u : 0xffff0000u);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+            }
+        }
     }
-    return x;
+    return !bad;
 }
 
 template <int kDtype, int kHalves>
-__device__ void load_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
+__device__ void row_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
     using R = Ring<kHalves>;
     const spec_tree_attention_t &a = g.a;
     const TileMap<kHalves> map;
-    int qs = 0, ks = 0, vs = 0;                          // slots, and the parity of their `empty` that means free
-    uint32_t qp = 1, kp = 1, vp = 1;
+    int qs = 0, ks = 0, vs = 0;
+    uint32_t qp = 1, kp = 1, vp = 1, boxes_parity = 0;
+    auto arrive_all_copied = [](uint64_t *bar) {
+#pragma unroll
+        for (int i = 0; i < kBoxWarps; ++i) arrive_when_copied(bar);
+    };
     Walk walk(g, sh);
     Unit u;
     while (walk.next(g, u)) {
@@ -405,73 +496,39 @@ __device__ void load_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint3
             arrive_when_copied(&sh->q_full[qs]);
             if (++qs == R::kQ) qs = 0, qp ^= 1;
         }
-        // K of a tile goes ahead of V of the tile before.  Tiles [t0, boxed) lie in the cache and come by TMA.
-        const int boxed = g.box_tokens ? min(u.t1, max(u.t0, u.len / kTileKeys)) : u.t0;
-        KeyPlace here, before;
-        int page = 0, page_before = 0;
-        auto look = [&](int t) {
-            if (t < boxed) page = box_page<kHalves>(g, u, t, map.warp, map.lane);
-            else if (t < u.t1) here = key_place(a, u, t * kTileKeys + map.own_row());
-        };
-        look(u.t0);
-        for (int t = u.t0; t <= u.t1; ++t) {
+        const int boxed = boxed_tiles(g, u);
+        pass_over<R::kK>(boxed - u.t0, ks, kp);
+        pass_over<R::kV>(boxed - u.t0, vs, vp);
+        if (boxed == u.t1) continue;
+        KeyPlace here = key_place(a, u, boxed * kTileKeys + map.own_row()), before = {};
+        if (!warp_wait(&sh->boxes_asked, boxes_parity, sh, a.err_word)) return;
+        boxes_parity ^= 1;
+        for (int t = boxed; t <= u.t1; ++t) {
             const KeyPlace now = here;
-            const int page_now = page;
             if (t < u.t1) {
-                look(t + 1);                             // (ahead of the wait)
+                if (t + 1 < u.t1) here = key_place(a, u, (t + 1) * kTileKeys + map.own_row());
                 if (!warp_wait(&sh->k_empty[ks], kp, sh, a.err_word)) return;
-                const uint32_t tile = k_tiles + ks * R::kBytes;
-                if (t < boxed) {
-                    load_boxes<kHalves>(g, &g.k_map, u, t, page_now, map.warp, tile, &sh->k_full[ks]);
-                } else {
-                    map.copy(tile, row_of(now, u.b, u.head, a.k_cache, a.kc_stride, a.k, a.k_stride), a.D);
-                    arrive_when_copied(&sh->k_full[ks]);
-                }
-                if (++ks == R::kK) ks = 0, kp ^= 1;
+                map.copy(k_tiles + ks * R::kBytes, row_of(now, u.b, u.head, a.k_cache, a.kc_stride, a.k, a.k_stride), a.D);
+                arrive_all_copied(&sh->k_full[ks]);
+                pass_over<R::kK>(1, ks, kp);
             }
-            if (t > u.t0) {
+            if (t > boxed) {
                 if (!warp_wait(&sh->v_empty[vs], vp, sh, a.err_word)) return;
+                if (t == u.t1 && map.lane == 0) mbar_arrive(&sh->rows_asked);
                 const uint32_t tile = v_tiles + vs * R::kBytes;
-                if (t - 1 < boxed) {
-                    load_boxes<kHalves>(g, &g.v_map, u, t - 1, page_before, map.warp, tile, &sh->v_full[vs]);
-                    if (++vs == R::kV) vs = 0, vp ^= 1;
-                    before = now;
-                    page_before = page_now;
-                    continue;
-                }
                 map.copy(tile, row_of(before, u.b, u.head, a.v_cache, a.vc_stride, a.v, a.v_stride), a.D);
-                const int key0 = (t - 1) * kTileKeys;
-                if (key0 + kTileKeys > u.len) {
-                    // Rows of the tree are not seen by every query, and 0 * inf would reach those that do not: what is not finite is
-                    // zero in the tile, and the unit's result takes it from memory (add_not_finite).
+                const int tree = u.len - (t - 1) * kTileKeys;            // the tree's first row
+                if (tree < kTileKeys) {
                     asm volatile("cp.async.wait_all;" ::: "memory");
-                    bool bad = false;
-                    if (map.chunk * 8 < a.D) {
-                        for (int i = 0; i < TileMap<kHalves>::kPasses; ++i) {
-                            const int r = map.row + i * TileMap<kHalves>::kStep;
-                            if (key0 + r < u.len || key0 + r >= u.len + u.nodes) continue;
-                            const uint32_t at = map.address(tile, r);
-                            uint32_t x[4];
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
-                            bool found = false;
-                            for (int e = 0; e < 4; ++e) x[e] = finite_or_zero<kDtype>(x[e], found);
-                            if (found)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                             ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-                            bad |= found;
-                        }
-                    }
-                    if (bad) sh->not_finite[u.index % kUnitFlags] = 1;
+                    if (!finite_values<kDtype>(map, tile, tree, tree + u.nodes, a.D)) sh->not_finite[u.index % kUnitFlags] = 1;
                     fence_async_proxy();
-                    mbar_arrive(&sh->v_full[vs]);
+                    mbar_arrive_n(&sh->v_full[vs], kBoxWarps);
                 } else {
-                    arrive_when_copied(&sh->v_full[vs]);
+                    arrive_all_copied(&sh->v_full[vs]);
                 }
-                if (++vs == R::kV) vs = 0, vp ^= 1;
+                pass_over<R::kV>(1, vs, vp);
             }
             before = now;
-            page_before = page_now;
         }
     }
 }
@@ -617,16 +674,18 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[128],
         : "r"(taddr) : "memory");
 #undef V
 }
-// 128 columns: the four loads are in flight together.  Nothing may use a register before the wait, so each passes through a
-// statement behind it.
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
-#pragma unroll
-    for (int c = 0; c < 128; c += 32) tmem_ld32_async(taddr + c, v, c);
+// Nothing may use a register before the wait, so each passes through a statement behind it.
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[128]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int c = 0; c < 128; c += 8)
         asm volatile("" : "+f"(v[c]), "+f"(v[c + 1]), "+f"(v[c + 2]), "+f"(v[c + 3]), "+f"(v[c + 4]), "+f"(v[c + 5]), "+f"(v[c + 6]),
                           "+f"(v[c + 7]));
+}
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 32) tmem_ld32_async(taddr + c, v, c);
+    tmem_ld_wait(v);
 }
 
 // Two lanes of fp32 arithmetic in one instruction.
@@ -643,31 +702,19 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return *(float2 *)&r;
 }
 
-// Scores that the row does not see become minus infinity.  A pass of its own over the few tiles that need it: as a variant of
-// softmax_tile it doubled the unrolled code, whose instructions then came from beyond the nearest caches (12000 cycles a tile).
-__device__ __forceinline__ void mask_tile(uint32_t s_addr, const uint32_t (&seen)[4]) {
-#pragma unroll 1
-    for (int c = 0; c < 8; ++c) {
-        const uint32_t bits = (c & 4 ? c & 2 ? seen[3] : seen[2] : c & 2 ? seen[1] : seen[0]) >> (c & 1) * 16;
-        if (__all_sync(0xffffffffu, (bits & 0xffffu) == 0xffffu)) continue;
-        float x[16];
-        uint32_t r[16];
-        tc::tmem_ld16(s_addr + c * 16, x);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = bits >> i & 1 ? __float_as_uint(x[i]) : 0xff800000u;
-        tmem_st16(s_addr + c * 16, r);
-    }
-    tmem_wait_st();
-}
-
 // One tile of a row: probabilities in place of the scores.  The maximum follows the tiles lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
 // saves nearly every pass over the accumulated output (a pass waits for the products of the tile before).
 template <int kDtype, int kHalves>
 __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
-                                             uint64_t *pv_done, uint32_t pv_parity, Row &row) {
+                                             uint64_t *pv_done, uint32_t pv_parity, bool masked, const uint32_t (&seen)[4], Row &row) {
     float x[128];
     tmem_ld128(s_addr, x);
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+            if (!(seen[i >> 5] >> (i & 31) & 1)) x[i] = -INFINITY;
+    }
     float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int i = 0; i < 128; i += 2) top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
@@ -716,8 +763,8 @@ __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint
     return true;
 }
 
-// What load_role kept out of the products: values that are not finite, of the nodes that the row sees, are added to the row's
-// result in memory, which its own thread has just written (columns col0 .. col0 + 31).
+// What finite_values kept out of the products: values that are not finite, of the nodes that the row sees, are added to the row's
+// result in memory, which its own thread has just written (columns col0 .. col0 + 63).
 template <int kDtype>
 __device__ __forceinline__ void add_not_finite(const spec_tree_attention_t &a, const Unit &u, const RowMask &mask, int col0,
                                             uint16_t *out, float *part) {
@@ -725,7 +772,7 @@ __device__ __forceinline__ void add_not_finite(const spec_tree_attention_t &a, c
     for (int n = first; n < end; ++n) {
         if (!(mask.bits(n) & 1)) continue;
         const uint16_t *v = (const uint16_t *)a.v + u.b * a.v_stride[0] + n * a.v_stride[1] + u.head * a.v_stride[2];
-        for (int i = col0; i < min(col0 + 32, a.D); ++i) {
+        for (int i = col0; i < min(col0 + 64, a.D); ++i) {
             const float x = number<kDtype>(v[i], 0);
             if (fabsf(x) < INFINITY) continue;
             if (part != nullptr) part[i] += x;
@@ -774,8 +821,8 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             tc_fence_after();
             if (active) {
                 const uint32_t o_addr = lanes + 256 + stream * 128, parity = (steps_done - 1) & 1;
-                if (masked) mask_tile(s_addr, seen);
-                const bool ok = softmax_tile<kDtype, kHalves>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream], parity, row);
+                const bool ok = softmax_tile<kDtype, kHalves>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream], parity, masked,
+                                                              seen, row);
                 if (!ok) return false;
             }
             first = false;
@@ -805,39 +852,39 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             uint16_t *out = (uint16_t *)a.out + u.b * a.out_stride[0] + node * a.out_stride[1] +
                             (u.head * g.group + head) * a.out_stride[2];
             const size_t part = ((size_t)(2 * blockIdx.x + (u.index ? 1 : 0))) * g.part_rows + r;
+            float *part_out = g.part_out + part * a.D;
+            const bool whole = u.whole();
+            w[0] *= inv;
+            w[1] *= inv;
+            // 64 columns at a time, of both streams, behind one wait: a load of TMEM takes several hundred cycles while MMAs run
 #pragma unroll 1
-            for (int c = two ? 0 : stream; c * 32 < a.D; c += two ? 1 : 2) {
-                float o[32];
-                tmem_ld32(lanes + 256 + (two ? stream * 128 : 0) + c * 32, o);
+            for (int c = two ? 0 : stream * 64; c < (two ? a.D : min(a.D, stream * 64 + 64)); c += 64) {
+                float o[128];
+                tmem_ld32_async(lanes + 256 + (two ? stream * 128 : 0) + c, o, 0);
+                tmem_ld32_async(lanes + 256 + (two ? stream * 128 : 0) + c + 32, o, 32);
+                tmem_ld32_async(lanes + 384 + c, o, 64);
+                tmem_ld32_async(lanes + 384 + c + 32, o, 96);
+                tmem_ld_wait(o);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] *= w[0];
-                if (join) {
-                    float o1[32];
-                    tmem_ld32(lanes + 384 + c * 32, o1);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = fmaf(o1[i], w[1], o[i]);
-                }
+                for (int i = 0; i < 64; ++i) o[i] = join ? fmaf(o[64 + i], w[1], o[i] * w[0]) : o[i] * w[0];
                 if (r < u.rows) {
-                    const int cols = a.D - c * 32;
-                    if (u.whole()) {
-                        uint4 *to = (uint4 *)(out + c * 32);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
+                    for (int i = 0; i < 64; i += 8) {
+                        if (c + i >= a.D) continue;
+                        if (whole) {
                             uint4 y;
-                            y.x = pack2<kDtype>(o[i] * inv, o[i + 1] * inv);
-                            y.y = pack2<kDtype>(o[i + 2] * inv, o[i + 3] * inv);
-                            y.z = pack2<kDtype>(o[i + 4] * inv, o[i + 5] * inv);
-                            y.w = pack2<kDtype>(o[i + 6] * inv, o[i + 7] * inv);
-                            if (i < cols) to[i / 8] = y;
+                            y.x = pack2<kDtype>(o[i], o[i + 1]);
+                            y.y = pack2<kDtype>(o[i + 2], o[i + 3]);
+                            y.z = pack2<kDtype>(o[i + 4], o[i + 5]);
+                            y.w = pack2<kDtype>(o[i + 6], o[i + 7]);
+                            *(uint4 *)(out + c + i) = y;
+                        } else {
+                            *(float4 *)(part_out + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                            *(float4 *)(part_out + c + i + 4) = make_float4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]);
                         }
-                    } else {
-                        float4 *to = (float4 *)(g.part_out + part * a.D + c * 32);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            if (i < cols) to[i / 4] = make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
                     }
+                    if (bad) add_not_finite<kDtype>(a, u, mask, c, out, whole ? nullptr : part_out);
                 }
-                if (bad && r < u.rows) add_not_finite<kDtype>(a, u, mask, c * 32, out, u.whole() ? nullptr : g.part_out + part * a.D);
                 __syncwarp();
             }
             if (r < u.rows && (two || stream == 0)) {
@@ -848,9 +895,11 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
         if (!softmax_meet(sh, meet, a.err_word)) return false;       // nobody writes O, stat or the flag while somebody may still read them
         if (threadIdx.x == 0) {
             sh->not_finite[u.index % kUnitFlags] = 0;
+            // where its last tile begins
+            const long long last = u.begin + (u.tiles == 1 ? 0 : sh->deal.unit_cost + ((long long)(u.tiles - 1) << (two ? 1 : 0)));
             if (u.t0 == 0 && !u.whole())
                 g.joins[blockIdx.x] = {u.b, u.head, u.row0, u.rows,
-                                       sh->deal.owner(u.begin + ((long long)(u.tiles - 1) << (two ? 1 : 0))) - (int)blockIdx.x + 1,
+                                       sh->deal.owner(last) - (int)blockIdx.x + 1,
                                        2 * (int)blockIdx.x + (u.index ? 1 : 0), {}};
         }
     }
@@ -874,15 +923,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             mbar_init(&sh->pv_done[i], 1);
         }
         for (int i = 0; i < R::kK; ++i) {
-            mbar_init(&sh->k_full[i], kLoadThreads);
+            mbar_init(&sh->k_full[i], kTileArrivals);
             mbar_init(&sh->k_empty[i], 1);
         }
         for (int i = 0; i < R::kV; ++i) {
-            mbar_init(&sh->v_full[i], kLoadThreads);
+            mbar_init(&sh->v_full[i], kTileArrivals);
             mbar_init(&sh->v_empty[i], 1);
         }
         mbar_init(&sh->meet, kSoftmaxThreads);
         mbar_init(&sh->drained, 1);
+        mbar_init(&sh->boxes_asked, kBoxWarps);
+        mbar_init(&sh->rows_asked, kLoadThreads / 32);
         sh->abort_flag = 0;
         for (int i = 0; i < kUnitFlags; ++i) sh->not_finite[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -917,12 +968,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (warp == 8 && tc::elect_one()) {
             mma_role<kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
             umma_commit(&sh->drained);                   // what was issued ends before TMEM and shared memory go
-            for (uint32_t it = 0; it < tc::kSpinMax && !mbar_try_wait(&sh->drained, 0); ++it) {}
+            for (uint32_t it = 0; it < kSpinMax && !mbar_try_wait(&sh->drained, 0); ++it) {}
         }
+        if (warp > 8) box_role<kHalves>(g, sh, k_tiles, v_tiles);
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        load_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
+        row_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
         asm volatile("cp.async.wait_all;" ::: "memory");
     }
     __syncwarp();
