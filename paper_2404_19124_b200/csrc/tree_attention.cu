@@ -32,7 +32,6 @@ namespace {
 using tc::ex2_approx;
 using tc::mbar_arrive;
 using tc::mbar_init;
-using tc::mbar_try_wait;
 using tc::smem_u32;
 using tc::tc_fence_after;
 using tc::tc_fence_before;
@@ -54,7 +53,8 @@ constexpr int kTileArrivals = kBoxWarps * kLoadThreads;
 constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
 constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns each
 constexpr int kUnitFlags = 8;
-constexpr uint32_t kSpinMax = 1u << 22;         // polls of a wait, 64 ns and more each, before it gives up
+constexpr uint64_t kWaitMaxNs = 1000000000;     // after which a wait gives up
+constexpr uint32_t kWaitHintNs = 20000;
 constexpr float kRescaleAbove = 8.f;            // see softmax_tile
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -118,20 +118,34 @@ struct AttnArgs {
     CUtensorMap k_map, v_map; // the caches as (column, token, head, page)
 };
 
-__device__ __forceinline__ bool poll(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
-    for (uint32_t it = 0; it < kSpinMax; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (it > tc::kSpinFast) {
-            if (sh->abort_flag) return false;
-            __nanosleep(64);
-        }
-    }
-    sh->abort_flag = 1;
-    report_error(err, SPEC_ERR_TIMEOUT);
-    return false;
+// Waits are bounded by time.  A try sleeps in hardware until the phase ends or the hint has passed: warps that poll take the issue
+// slots that the softmax needs.
+__device__ __forceinline__ bool try_wait(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(kWaitHintNs) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
 }
 __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
-    return mbar_try_wait(bar, parity) || poll(bar, parity, sh, err);
+    if (try_wait(bar, parity)) return true;
+    const uint64_t start = now_ns();
+    while (!try_wait(bar, parity)) {
+        if (sh->abort_flag) return false;
+        if (now_ns() - start > kWaitMaxNs) {
+            sh->abort_flag = 1;
+            report_error(err, SPEC_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
 }
 // The whole warp waits, leaves converged and with one verdict.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Shared *sh, int32_t *err) {
@@ -968,7 +982,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (warp == 8 && tc::elect_one()) {
             mma_role<kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
             umma_commit(&sh->drained);                   // what was issued ends before TMEM and shared memory go
-            for (uint32_t it = 0; it < kSpinMax && !mbar_try_wait(&sh->drained, 0); ++it) {}
+            for (const uint64_t start = now_ns(); !try_wait(&sh->drained, 0) && now_ns() - start < kWaitMaxNs;) {}
         }
         if (warp > 8) box_role<kHalves>(g, sh, k_tiles, v_tiles);
         __syncwarp();
