@@ -153,6 +153,9 @@ if _pycall is not None:
     _pycall.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.spec_verify, _lib.spec_verify_early, _lib.spec_next_ctx,
                                                          _lib.spec_draft)),
                  torch.int32, torch.bfloat16, torch.float32, _current_device, _current_raw_stream)
+    _pycall.bind_tree(*(C.cast(f, C.c_void_p).value for f in (_lib.spec_tree_plan, _lib.spec_page_tables,
+                                                              _lib.spec_tree_attention, _lib.spec_verify_tree,
+                                                              _lib.spec_kv_commit)), torch.float16, torch.int64)
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]):
@@ -536,6 +539,12 @@ def _err_ptr(err_workspace: Optional[torch.Tensor], device: torch.device):
 def spec_tree_plan(cand_tok: torch.Tensor, last_tok: torch.Tensor, seq_len: torch.Tensor, T: int,
                    tree: Optional[SpecTree] = None, stream: Optional[torch.cuda.Stream] = None) -> SpecTree:
     """The candidates [B, K, n] of every sequence as one tree of at most T nodes, shared prefixes once."""
+    if _pycall is not None and tree is not None:
+        status = _pycall.tree_plan(cand_tok, last_tok, seq_len, T, *tree, stream)
+        if status is not None:
+            if status != SPEC_OK:
+                raise SpecError(status, "spec_tree_plan")
+            return tree
     dev = _cuda_device(cand_tok, "cand_tok")
     B, K, n = cand_tok.shape
     T = int(T)
@@ -558,6 +567,14 @@ def spec_page_tables(seq_len: torch.Tensor, n_new: Optional[torch.Tensor], block
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Grows block_table [B, max_pages] for seq_len + n_new tokens (n_new None: max_new everywhere) from the end of free_pages;
     returns slots, int64 [B, max_new].  n_pages [B] and free_count [1] are updated in place unless outputs for them are given."""
+    if _pycall is not None and slots is not None and err_workspace is None and max_new is None:
+        status = _pycall.page_tables(seq_len, n_new, block_table, n_pages, free_pages, free_count, page_size, slots,
+                                     n_pages if n_pages_out is None else n_pages_out,
+                                     free_count if free_count_out is None else free_count_out, stream)
+        if status is not None:
+            if status != SPEC_OK:
+                raise SpecError(status, "spec_page_tables")
+            return slots
     dev = _cuda_device(seq_len, "seq_len")
     i32, (B,) = torch.int32, seq_len.shape
     if max_new is None:
@@ -599,6 +616,13 @@ def spec_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cac
     """q [B, T, Hq, D] over the cache [pages, page_size, Hkv, D] (any strides but a dense last dimension; a cache kept as
     [pages, Hkv, page_size, D] is passed transposed) and the tree's own k, v [B, T, Hkv, D].  mask: SpecTree.mask, None for
     chains; scale: D ** -0.5 by default.  Returns out; lse (fp32 [B, T, Hq]) is written when given."""
+    if _pycall is not None and out is not None and workspace is not None and err_workspace is None:
+        status = _pycall.tree_attention(q, k, v, k_cache, v_cache, block_table, seq_len, mask, n_nodes,
+                                        q.shape[-1] ** -0.5 if scale is None else scale, out, lse, workspace, stream)
+        if status is not None:
+            if status != SPEC_OK:
+                raise SpecError(status, "spec_tree_attention")
+            return out
     dev = _cuda_device(q, "q")
     dt, i32 = q.dtype, torch.int32
     if dt != torch.bfloat16 and dt != torch.float16:
@@ -607,7 +631,6 @@ def spec_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cac
     Hkv = k.shape[2]
     pages, page_size = k_cache.shape[:2]
     max_pages = block_table.shape[1]
-    made = out is None
     out = _made(out, (B, T, Hq, D), dt, dev, stream)
     if workspace is None:
         need = spec_tree_attention_workspace_bytes(B, T, Hq, Hkv, D)
@@ -643,6 +666,14 @@ def spec_verify_tree(tok: torch.Tensor, parent: torch.Tensor, n_nodes: torch.Ten
                      stream: Optional[torch.cuda.Stream] = None):
     """Greedy walk down the trees by logits [B, T, V] (bf16, fp16 or fp32; a dense last dimension), at most n tokens deep (n
     None: as long as path).  Returns (accept_len, last_node, next_tok, path).  Penalties need hist_tok and hist_len."""
+    if (_pycall is not None and path is not None and next_tok is not None and last_node is not None and accept_len is not None and
+            (n is None or n == path.shape[1] - 1)):
+        status = _pycall.verify_tree(tok, parent, n_nodes, logits, hist_tok, hist_len, prompt_len, repetition, frequency, presence,
+                                     bias_tok, bias_val, bias_len, allow, accept_len, last_node, next_tok, path, stream)
+        if status is not None:
+            if status != SPEC_OK:
+                raise SpecError(status, "spec_verify_tree")
+            return accept_len, last_node, next_tok, path
     dev = _cuda_device(logits, "logits")
     i32, f32 = torch.int32, torch.float32
     if logits.dtype not in _DTYPES:
@@ -677,6 +708,12 @@ def spec_kv_commit(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
                    stream: Optional[torch.cuda.Stream] = None) -> None:
     """Copies the accepted path's rows of k, v [L, B, T, H, D] to the slots [B, n + 1] of the caches [L, pages, page_size, H, D];
     new_len (may be seq_len) receives seq_len + accept_len + 1."""
+    if _pycall is not None and err_workspace is None:
+        status = _pycall.kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, stream)
+        if status is not None:
+            if status != SPEC_OK:
+                raise SpecError(status, "spec_kv_commit")
+            return
     dev = _cuda_device(k, "k")
     dt, i32 = k.dtype, torch.int32
     if dt.itemsize != 2:
