@@ -420,7 +420,9 @@ int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace
  *   allow        dev uint32 [B, T, ceil(V / 32)], bit set: the token is allowed; NULL: all are
  *   accept_len, last_node, next_tok  dev int32 [B] (out)   tokens accepted, last node of the path, g behind it
  *   path         dev int32 [B, n + 1] (out)   nodes of the path, path[.., 0] = 0; -1 behind it
- * List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 gets accept_len 0 and -1 elsewhere. */
+ * Limits: T <= SPEC_MAX_TREE_NODES; the tokens that penalties and biases touch have to fit a table of 200 KB per CTA, which
+ * holds any for V up to 390000 (270000 with penalties and biases), and histories of 10000 tokens for V of millions; else
+ * SPEC_ERR_SHAPE.  List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 gets accept_len 0 and -1 elsewhere. */
 typedef struct {
     int32_t logits_dtype, B, T, V, n, max_hist, max_bias;
     const int32_t *tok, *parent, *n_nodes;
@@ -445,7 +447,7 @@ int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
  *   path         dev int32 [B, n + 1], accept_len dev int32 [B]   as spec_verify_tree writes them
  *   slots        dev int64 [B, n + 1]   as spec_page_tables writes them for max_new = n + 1
  *   seq_len, new_len  dev int32 [B]; new_len may be seq_len, or NULL
- * accept_len beyond n is taken as n, below 0 nothing is copied.  A node outside [0, T) or a slot outside the cache is not copied, and
+ * Caches of more than 2^31 - 1 tokens a layer: SPEC_ERR_SHAPE.  accept_len beyond n is taken as n, below 0 nothing is copied.  A node outside [0, T) or a slot outside the cache is not copied, and
  * err_word receives SPEC_ERR_INDEX_RANGE. */
 typedef struct {
     int32_t L, B, T, n, H, D, page_size, n_pages;

@@ -246,32 +246,36 @@ __global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(const TableArg
 }
 
 // ---- the greedy walk -----------------------------------------------------------------------------------------------
-// A cluster of CTAs per sequence, each with a part of the vocabulary.  Per step: every CTA finds the maximum of its part of the
-// current node's row, the CTAs exchange theirs through distributed shared memory, and all of them look up the child
-// that carries the winner.  Only the rows on the path are read.  The constraints apply to what is read: the tokens of a
-// CTA's part that penalties or biases touch are counted in shared memory once and marked in a bitmap, so that a vector
-// of logits without a marked token costs what it costs without constraints.
-constexpr int kWalkThreads = 512;
+// A cluster of CTAs per sequence; the vocabulary goes to them in blocks of 4096 tokens in turn.  Per step every CTA finds the
+// maximum of its blocks of the current node's row, the CTAs exchange theirs through distributed shared memory, and all of them
+// look up the child that carries the winner.  Only the rows on the path are read, so a step is latency: loads of four vectors
+// per thread in flight, one exchange, one look at the tree, which lies in shared memory.
+//
+// Constraints.  The tokens that penalties or biases touch are few.  Each CTA counts those of its blocks once, in a table in
+// shared memory, and marks them in a bitmap: the pass over the row leaves them out (and what the grammar forbids), and every
+// listed token is looked at by itself.  The table is hashed while that is smaller, which lets four CTAs share an SM for
+// histories of a few thousand tokens (64 sequences of a vocabulary of 128256, histories of up to 2048: 278 us with a dense table of
+// 130 KB and per-element checks), else it has an entry per token.
+constexpr int kWalkThreads = 256;
 constexpr int kWalkWarps = kWalkThreads / 32;
-constexpr int kWalkMaxCluster = 8;
+constexpr int kWalkCtasPerSm = 4;            // by registers
+constexpr int kWalkMaxCluster = 16;
+constexpr int kBlockTokens = 4096;
 constexpr int kNoToken = INT_MAX;
 constexpr uint32_t kSeen = 1u << 31;         // of a token's count: it is in the history (the rest: times it was generated)
+constexpr uint32_t kFree = 0xffffffffu;      // of a key
 
 struct WalkArgs {
     spec_tree_verify_t v;
-    int part;                                // vocabulary entries of a CTA, a multiple of 32
-    int pass;                                // ... that its tables in shared memory cover at a time, a multiple of 32
+    int log_ctas;
+    int cap;                                 // entries of the table: a power of two (hashed) or the CTA's tokens; 0: no constraints by token
+    int hashed, max_list, part;              // part: tokens of a CTA, whole blocks
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
 __device__ __forceinline__ void cluster_sync() {
@@ -292,6 +296,7 @@ template <> struct Logit<SPEC_BF16> {
         const uint32_t w = (&v.x)[i >> 1];
         return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
     }
+    static __device__ __forceinline__ float at(const void *row, int i) { return bf16_bits_to_float(((const uint16_t *)row)[i]); }
 };
 template <> struct Logit<SPEC_F16> {
     static constexpr int kBytes = 2;
@@ -299,10 +304,14 @@ template <> struct Logit<SPEC_F16> {
         const uint32_t w = (&v.x)[i >> 1];
         return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w >> 16 : w & 0xffffu)));
     }
+    static __device__ __forceinline__ float at(const void *row, int i) {
+        return __half2float(__ushort_as_half(((const unsigned short *)row)[i]));
+    }
 };
 template <> struct Logit<SPEC_F32> {
     static constexpr int kBytes = 4;
     static __device__ __forceinline__ float get(const uint4 &v, int i) { return __uint_as_float((&v.x)[i]); }
+    static __device__ __forceinline__ float at(const void *row, int i) { return ((const float *)row)[i]; }
 };
 
 struct Best {
@@ -315,61 +324,188 @@ struct Best {
             tok = t;
         }
     }
+    __device__ __forceinline__ void join_warp() {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            const float ov = __shfl_xor_sync(0xffffffffu, value, off);
+            const int ot = __shfl_xor_sync(0xffffffffu, tok, off);
+            offer(ov, ot);
+        }
+    }
 };
 
-// Tables of one pass over a part of the vocabulary.
-struct WalkTables {
-    uint32_t *count;      // [pass] kSeen and the times generated
-    uint32_t *bias;       // [pass] entry of the bias list + 1, 0: none
-    uint32_t *marked;     // [pass / 32]
+// The tokens of this CTA that penalties or biases touch.
+struct WalkTable {
+    uint32_t *key;        // [cap] hashed only: token, kFree
+    uint32_t *count;      // [cap] kSeen and the times generated
+    uint32_t *bias;       // [cap] entry of the bias list + 1, 0: none
+    uint32_t *marked;     // [part / 32]
+    int *list;            // [max_list] entries in use
+    int *n_list;
 };
 
-__device__ __forceinline__ void walk_count(const WalkTables &w, int t, bool generated) {
-    atomicOr(&w.marked[t >> 5], 1u << (t & 31));
-    atomicOr(&w.count[t], kSeen);
-    if (generated) atomicAdd(&w.count[t], 1u);
+// Number of a token among the CTA's own.
+__device__ __forceinline__ int local_token(const WalkArgs &a, int t) {
+    return (t / kBlockTokens >> a.log_ctas) * kBlockTokens + t % kBlockTokens;
+}
+__device__ __forceinline__ bool owns(const WalkArgs &a, uint32_t rank, int t) {
+    return (unsigned)t < (unsigned)a.v.V && (t / kBlockTokens & ((1 << a.log_ctas) - 1)) == (int)rank;
 }
 
-__device__ __forceinline__ float walk_adjust(const WalkArgs &a, const WalkTables &w, int b, int t, float x, float rep,
-                                             float freq, float pres) {
+// The entry of a token, which is made and listed if there is none.
+__device__ __forceinline__ int table_entry(const WalkArgs &a, const WalkTable &w, int t) {
+    const int local = local_token(a, t);
+    int at = local;
+    if (a.hashed) {
+        at = (int)((uint32_t)t * 0x9e3779b1u >> 8) & (a.cap - 1);
+        for (;;) {                                       // there are fewer tokens than entries
+            const uint32_t was = atomicCAS(&w.key[at], kFree, (uint32_t)t);
+            if (was == kFree || was == (uint32_t)t) break;
+            at = (at + 1) & (a.cap - 1);
+        }
+    }
+    const uint32_t bit = 1u << (local & 31);
+    if (!(atomicOr(&w.marked[local >> 5], bit) & bit)) w.list[atomicAdd(w.n_list, 1)] = at;
+    return at;
+}
+
+__device__ __forceinline__ float walk_adjust(const WalkArgs &a, const WalkTable &w, int b, int at, float x, float rep, float freq,
+                                             float pres) {
     // Each step rounds once, in the order of the definition: no contraction into fused multiply-adds.
     if (a.v.hist_tok != nullptr) {
-        const uint32_t c = w.count[t];
+        const uint32_t c = w.count[at];
         if (c & kSeen) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
         const uint32_t times = c & ~kSeen;
         if (times) x = __fsub_rn(__fsub_rn(x, __fmul_rn(freq, (float)times)), pres);
     }
-    if (a.v.bias_tok != nullptr && w.bias[t])
-        x = __fadd_rn(x, a.v.bias_val[(size_t)b * a.v.max_bias + w.bias[t] - 1]);
+    if (a.v.bias_tok != nullptr && w.bias[at]) x = __fadd_rn(x, a.v.bias_val[(size_t)b * a.v.max_bias + w.bias[at] - 1]);
     return x;
 }
 
+// Bits of n <= 8 consecutive positions of a bit field, from `first` on.
+__device__ __forceinline__ uint32_t bits_from(const uint32_t *field, int first, int words) {
+    const int w = first >> 5;
+    return __funnelshift_r(field[w], w + 1 < words ? field[w + 1] : 0u, first & 31);
+}
+
+// Elements [begin, end) of a row: those that `allow` (null: all) and not `skip` (null: none; bits of the elements from skip0 on) leave.
 template <int kDtype>
-__global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(const WalkArgs a) {
+__device__ __forceinline__ void scan_block(const char *row, int V, int begin, int end, const uint32_t *allow, int words,
+                                           const uint32_t *skip, int skip0, int skip_words, Best &best) {
+    constexpr int kPer = 16 / Logit<kDtype>::kBytes, kUnroll = 4;
+    const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);       // elements behind a vector's start
+    const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
+    const int v0 = (begin + skew) / kPer, v1 = (end + skew + kPer - 1) / kPer;
+    for (int i0 = v0 + threadIdx.x; i0 < v1; i0 += kWalkThreads * kUnroll) {
+        uint4 x[kUnroll];
+        uint32_t use[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int i = i0 + k * kWalkThreads, e0 = i * kPer - skew;
+            use[k] = 0;
+            if (i >= v1) continue;
+            // a vector that reaches beyond the row is read element by element: the memory there may be nobody's
+            if (e0 >= 0 && e0 + kPer <= V) {
+                x[k] = __ldg(vec + i);
+            } else {
+                uint32_t y[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    if (e0 + e < 0 || e0 + e >= V) continue;
+                    if (Logit<kDtype>::kBytes == 2) y[e / 2] |= (uint32_t)((const uint16_t *)row)[e0 + e] << 16 * (e % 2);
+                    else y[e] = ((const uint32_t *)row)[e0 + e];
+                }
+                x[k] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            uint32_t m = (1u << kPer) - 1;
+            if (e0 < begin) m &= m << (begin - e0);
+            if (e0 + kPer > end) m &= (1u << kPer) - 1 >> (e0 + kPer - end);
+            const int from = max(e0, begin), shift = from - e0;
+            if (allow != nullptr) m &= bits_from(allow, from, words) << shift;
+            if (skip != nullptr) m &= ~(bits_from(skip, from - skip0, skip_words) << shift);
+            use[k] = m;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int e0 = (i0 + k * kWalkThreads) * kPer - skew;
+            if (use[k] == 0) continue;
+            float top = -INFINITY;
+            int pos = 0;
+#pragma unroll
+            for (int e = kPer - 1; e >= 0; --e) {        // downwards: of equal ones the first stays
+                const float y = fmaxf(Logit<kDtype>::get(x[k], e), -INFINITY);       // (a NaN counts as minus infinity)
+                const bool take = (use[k] >> e & 1) && y >= top;
+                top = take ? y : top;
+                pos = take ? e : pos;
+            }
+            best.offer(top, e0 + pos);
+        }
+    }
+}
+
+template <int kDtype>
+__global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel(const WalkArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Best warp_best[kWalkWarps];
     __shared__ __align__(8) Best peer_best[2][kWalkMaxCluster];
-    __shared__ int went[SPEC_MAX_TREE_DEPTH];     // tokens taken so far
-    __shared__ int child;
+    __shared__ int child[3], n_list;                     // child: of three steps in turn, so that none is cleared while it is read
     griddep_launch();
     griddep_wait();
-    constexpr int kPer = 16 / Logit<kDtype>::kBytes;
-    const int t = threadIdx.x, lane = t & 31;
-    const uint32_t rank = cluster_rank(), ranks = cluster_size();
-    const int b = blockIdx.x / ranks;
     const spec_tree_verify_t &v = a.v;
-    const int V = v.V, lo = min((int)rank * a.part, V), hi = min(lo + a.part, V);
-    const bool listed = v.hist_tok != nullptr || v.bias_tok != nullptr;
-    WalkTables w;
-    w.count = (uint32_t *)smem;
-    w.bias = w.count + (v.hist_tok != nullptr ? a.pass : 0);
-    w.marked = w.bias + (v.bias_tok != nullptr ? a.pass : 0);
+    const int t = threadIdx.x, lane = t & 31, ranks = 1 << a.log_ctas;
+    const uint32_t rank = cluster_rank();
+    const int b = blockIdx.x >> a.log_ctas;
+    const int V = v.V, words = (V + 31) / 32;
+    int *tok = (int *)smem, *parent = tok + v.T;
+    WalkTable w;
+    w.key = (uint32_t *)(parent + v.T);
+    w.count = w.key + (a.hashed ? a.cap : 0);
+    w.bias = w.count + (v.hist_tok != nullptr ? a.cap : 0);
+    w.marked = w.bias + (v.bias_tok != nullptr ? a.cap : 0);
+    w.list = (int *)(w.marked + (a.cap ? a.part / 32 : 0));
+    w.n_list = &n_list;
     const int nodes = min(v.n_nodes[b], v.T);
     const float rep = v.repetition != nullptr ? v.repetition[b] : 1.f;
     const float freq = v.frequency != nullptr ? v.frequency[b] : 0.f;
     const float pres = v.presence != nullptr ? v.presence[b] : 0.f;
-    const int32_t *tok = v.tok + (size_t)b * v.T, *parent = v.parent + (size_t)b * v.T;
-    const int words = (V + 31) / 32;
+    for (int i = t; i < nodes; i += kWalkThreads) {
+        tok[i] = v.tok[(size_t)b * v.T + i];
+        parent[i] = v.parent[(size_t)b * v.T + i];
+    }
+    if (t == 0) {
+        n_list = 0;
+        child[0] = INT_MAX;
+    }
+    if (a.cap) {
+        if (a.hashed)
+            for (int i = t; i < a.cap; i += kWalkThreads) w.key[i] = kFree;
+        for (uint32_t *p = w.count + t; p < (uint32_t *)w.list; p += kWalkThreads) *p = 0;
+        __syncthreads();
+        if (v.hist_tok != nullptr) {
+            const int size = min(v.hist_len[b], v.max_hist), prompt = v.prompt_len == nullptr ? 0 : v.prompt_len[b];
+            const int32_t *hist = v.hist_tok + (size_t)b * v.max_hist;
+            for (int i0 = 0; i0 < size; i0 += kWalkThreads) {
+                const int i = i0 + t, h = i < size ? hist[i] : -1;
+                const bool mine = i < size && owns(a, rank, h);
+                // equal tokens of a warp are counted together: a few tokens make up most of a text
+                const unsigned same = __match_any_sync(0xffffffffu, mine ? h : -1);
+                const unsigned made = __ballot_sync(0xffffffffu, mine && i >= prompt) & same;
+                if (mine && lane == __ffs(same) - 1) {
+                    const int at = table_entry(a, w, h);
+                    atomicOr(&w.count[at], kSeen);
+                    if (made) atomicAdd(&w.count[at], (uint32_t)__popc(made));
+                }
+            }
+        }
+        if (v.bias_tok != nullptr) {
+            const int size = v.bias_len == nullptr ? v.max_bias : min(v.bias_len[b], v.max_bias);
+            for (int i = t; i < size; i += kWalkThreads) {
+                const int h = v.bias_tok[(size_t)b * v.max_bias + i];
+                if (owns(a, rank, h)) atomicMax(&w.bias[table_entry(a, w, h)], (uint32_t)i + 1);     // the list's last entry counts
+            }
+        }
+    }
+    __syncthreads();
 
     int cur = 0, accepted = 0, token = -1;
     if (nodes > 0) {
@@ -378,95 +514,44 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(const WalkArgs 
             const char *row = (const char *)v.logits + ((long long)b * v.logits_stride[0] + (long long)cur * v.logits_stride[1]) *
                                                            Logit<kDtype>::kBytes;
             const uint32_t *allow = v.allow == nullptr ? nullptr : v.allow + ((size_t)b * v.T + cur) * words;
-            const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);   // elements behind a vector's start
-            const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
-            for (int p0 = lo; p0 < hi; p0 += a.pass) {
-                const int p1 = min(p0 + a.pass, hi);
-                if (listed && (step == 0 || a.pass < a.part)) {
-                    const int all = (v.hist_tok != nullptr ? a.pass : 0) + (v.bias_tok != nullptr ? a.pass : 0) + a.pass / 32;
-                    __syncthreads();
-                    for (int i = t; i < all; i += kWalkThreads) ((uint32_t *)smem)[i] = 0;
-                    __syncthreads();
-                    if (v.hist_tok != nullptr) {
-                        const int size = min(v.hist_len[b], v.max_hist), prompt = v.prompt_len == nullptr ? 0 : v.prompt_len[b];
-                        const int32_t *hist = v.hist_tok + (size_t)b * v.max_hist;
-                        for (int i = t; i < size + step; i += kWalkThreads) {
-                            const int h = i < size ? hist[i] : went[i - size];
-                            if (h >= p0 && h < p1) walk_count(w, h - p0, i >= prompt || i >= size);
-                        }
-                    }
-                    if (v.bias_tok != nullptr) {
-                        const int size = v.bias_len == nullptr ? v.max_bias : min(v.bias_len[b], v.max_bias);
-                        for (int i = t; i < size; i += kWalkThreads) {
-                            const int h = v.bias_tok[(size_t)b * v.max_bias + i];
-                            if (h < p0 || h >= p1) continue;
-                            atomicOr(&w.marked[(h - p0) >> 5], 1u << ((h - p0) & 31));
-                            atomicMax(&w.bias[h - p0], (uint32_t)i + 1);     // the list's last entry counts
-                        }
-                    }
-                    __syncthreads();
-                }
-                // vectors that hold elements of [p0, p1); the row's first and last one may reach beyond it into memory that belongs
-                // to other rows or to nobody, so those are read element by element
-                const int v0 = (p0 + skew) / kPer, v1 = (p1 + skew + kPer - 1) / kPer;
-                for (int i = v0 + t; i < v1; i += kWalkThreads) {
-                    const int e0 = i * kPer - skew;
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (e0 >= 0 && e0 + kPer <= V) {
-                        x = __ldg(vec + i);
-                    } else {
-                        for (int e = max(e0, 0); e < min(e0 + kPer, V); ++e) {
-                            if (Logit<kDtype>::kBytes == 2) ((uint16_t *)&x)[e - e0] = ((const uint16_t *)row)[e];
-                            else (&x.x)[e - e0] = ((const uint32_t *)row)[e];
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e) {
-                        const int at = e0 + e;
-                        if (at < p0 || at >= p1) continue;
-                        if (allow != nullptr && !(allow[at >> 5] >> (at & 31) & 1)) continue;
-                        float y = Logit<kDtype>::get(x, e);
-                        if (listed && (w.marked[(at - p0) >> 5] >> ((at - p0) & 31) & 1))
-                            y = walk_adjust(a, w, b, at - p0, y, rep, freq, pres);
-                        best.offer(y, at);
-                    }
+            for (int block = rank, local = 0; block * kBlockTokens < V; block += ranks, local += kBlockTokens)
+                scan_block<kDtype>(row, V, block * kBlockTokens, min((block + 1) * kBlockTokens, V), allow, words,
+                                   a.cap ? w.marked : nullptr, block * kBlockTokens - local, a.part / 32, best);
+            if (a.cap) {
+                const int n = n_list;
+                for (int i = t; i < n; i += kWalkThreads) {
+                    const int at = w.list[i];
+                    const int h = a.hashed ? (int)w.key[at]
+                                           : ((at / kBlockTokens << a.log_ctas) + (int)rank) * kBlockTokens + at % kBlockTokens;
+                    if (allow == nullptr || (allow[h >> 5] >> (h & 31) & 1))
+                        best.offer(walk_adjust(a, w, b, at, Logit<kDtype>::at(row, h), rep, freq, pres), h);
                 }
             }
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) {
-                const float ov = __shfl_xor_sync(0xffffffffu, best.value, off);
-                const int ot = __shfl_xor_sync(0xffffffffu, best.tok, off);
-                best.offer(ov, ot);
-            }
+            best.join_warp();
             if (lane == 0) warp_best[t >> 5] = best;
-            if (t == 0) child = INT_MAX;
+            if (t == 0) child[(step + 1) % 3] = INT_MAX;
             __syncthreads();
             if (t < 32) {
                 best = t < kWalkWarps ? warp_best[t] : Best{-INFINITY, kNoToken};
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) {
-                    const float ov = __shfl_xor_sync(0xffffffffu, best.value, off);
-                    const int ot = __shfl_xor_sync(0xffffffffu, best.tok, off);
-                    best.offer(ov, ot);
-                }
+                best.join_warp();
                 if (t < ranks) store_peer(&peer_best[step & 1][rank], t, best.value, best.tok);
             }
             cluster_sync();
-            best = {-INFINITY, kNoToken};
-            for (int r = 0; r < (int)ranks; ++r) best.offer(peer_best[step & 1][r].value, peer_best[step & 1][r].tok);
+            best = lane < ranks ? peer_best[step & 1][lane] : Best{-INFINITY, kNoToken};
+            best.join_warp();
             token = best.tok == kNoToken ? -1 : best.tok;
             if (rank == 0 && t == 0) v.path[(size_t)b * (v.n + 1) + step] = cur;
             if (step == v.n || token < 0) break;
             for (int i = 1 + t; i < nodes; i += kWalkThreads)
-                if (parent[i] == cur && tok[i] == token) atomicMin(&child, i);
-            if (t == 0) went[step] = token;
-            if (v.hist_tok != nullptr && a.pass >= a.part && t == 0 && token >= lo && token < hi)
-                walk_count(w, token - lo, true);
+                if (parent[i] == cur && tok[i] == token) atomicMin(&child[step % 3], i);
+            if (v.hist_tok != nullptr && t == 0 && owns(a, rank, token)) {
+                uint32_t *count = &w.count[table_entry(a, w, token)];
+                *count = (*count | kSeen) + 1;
+            }
             __syncthreads();
-            if (child == INT_MAX) break;
-            cur = child;
+            if (child[step % 3] == INT_MAX) break;
+            cur = child[step % 3];
             ++accepted;
-            __syncthreads();
         }
     }
     cluster_sync();                          // no CTA leaves while another may still write to its shared memory
@@ -481,7 +566,16 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(const WalkArgs 
 }
 
 // ---- accepted keys and values --------------------------------------------------------------------------------------
+// A thread copies 16 bytes of every accepted row, the loads of eight rows in flight before the first store: bound by HBM
+// for batches, by latency for few sequences.
 constexpr int kCommitThreads = 256;
+constexpr int kCommitRows = 8;
+
+__device__ __forceinline__ uint4 ld_once(const uint4 *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv_commit_t c) {
     griddep_launch();
@@ -499,24 +593,63 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv
     const uint16_t *src = (const uint16_t *)(is_v ? c.v : c.k) + layer * ss[0] + b * ss[1] + head * ss[3] + d;
     uint16_t *dst = (uint16_t *)(is_v ? c.v_cache : c.k_cache) + layer * ds[0] + head * ds[3] + d;
     const int rows = min(c.accept_len[b], c.n) + 1;
-    for (int j = 0; j < rows; ++j) {
-        const int node = c.path[(size_t)b * n1 + j];
-        const long long slot = c.slots[(size_t)b * n1 + j];
-        if (node < 0 || node >= c.T || slot < 0 || slot >= (long long)c.n_pages * c.page_size) {
-            report_error(c.err_word, SPEC_ERR_INDEX_RANGE);
-            continue;
+    for (int j0 = 0; j0 < rows; j0 += kCommitRows) {
+        uint4 x[kCommitRows];
+        uint16_t *to[kCommitRows];
+#pragma unroll
+        for (int i = 0; i < kCommitRows; ++i) {
+            to[i] = nullptr;
+            if (j0 + i >= rows) continue;
+            const int node = c.path[(size_t)b * n1 + j0 + i];
+            const long long slot = c.slots[(size_t)b * n1 + j0 + i];
+            if (node < 0 || node >= c.T || slot < 0 || slot >= (long long)c.n_pages * c.page_size) {
+                report_error(c.err_word, SPEC_ERR_INDEX_RANGE);
+                continue;
+            }
+            x[i] = ld_once((const uint4 *)(src + node * ss[2]));
+            const unsigned page = (unsigned)slot / (unsigned)c.page_size;
+            to[i] = dst + page * ds[1] + ((int)slot - (int)(page * c.page_size)) * ds[2];
         }
-        const uint4 x = *(const uint4 *)(src + node * ss[2]);
-        const long long page = slot / c.page_size;
-        *(uint4 *)(dst + page * ds[1] + (slot - page * c.page_size) * ds[2]) = x;
+#pragma unroll
+        for (int i = 0; i < kCommitRows; ++i)
+            if (to[i] != nullptr) *(uint4 *)to[i] = x[i];
     }
 }
 
 template <int kDtype>
-int launch_walk(const WalkArgs &a, int ctas, size_t smem, cudaStream_t st) {
-    SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_walk_kernel<kDtype>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    SPEC_CUDA_TRY(launch_pdl_cluster(tree_walk_kernel<kDtype>, dim3(ctas * a.v.B), dim3(kWalkThreads), smem, ctas, st, a));
+int launch_walk(const WalkArgs &a, size_t smem, cudaStream_t st) {
+    auto kernel = tree_walk_kernel<kDtype>;
+    const int ctas = 1 << a.log_ctas;
+    SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (ctas > 8) SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    SPEC_CUDA_TRY(launch_pdl_cluster(kernel, dim3((unsigned)ctas * a.v.B), dim3(kWalkThreads), smem, ctas, st, a));
     return SPEC_OK;
+}
+
+// The table of a CTA (bytes per entry: key, count, bias), the bitmap and the list.
+bool plan_walk_table(WalkArgs &a, int log_ctas, size_t &smem) {
+    const spec_tree_verify_t &v = a.v;
+    constexpr size_t kMost = 200 * 1024;
+    const long long blocks = ((long long)v.V + kBlockTokens - 1) / kBlockTokens;
+    const long long part = (blocks + (1 << log_ctas) - 1) / (1 << log_ctas) * kBlockTokens;
+    const size_t tree = (size_t)v.T * 8, per_entry = 4 * ((v.hist_tok ? 1 : 0) + (v.bias_tok ? 1 : 0));
+    a.log_ctas = log_ctas;
+    a.cap = a.hashed = a.max_list = a.part = 0;
+    smem = tree;
+    if (!per_entry) return true;
+    const long long tokens = (long long)v.max_hist + v.max_bias + v.n;
+    const long long listed = tokens < part ? tokens : part;
+    long long cap = 256;
+    while (cap * 3 < listed * 4) cap *= 2;               // three quarters full at most
+    const bool hashed = cap * (per_entry + 4) < part * per_entry;
+    if (!hashed) cap = part;
+    smem = tree + (size_t)cap * (per_entry + (hashed ? 4 : 0)) + (size_t)part / 8 + (size_t)listed * 4;
+    if (smem > kMost) return false;
+    a.cap = (int)cap;
+    a.hashed = hashed;
+    a.max_list = (int)listed;
+    a.part = (int)part;
+    return true;
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -539,7 +672,7 @@ int spec_tree_plan(const int32_t *cand_tok, const int32_t *last_tok, const int32
     const PlanSmem lay = plan_smem(K, n, T);
     if (lay.total > 40 * 1024)
         SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lay.total));
-    int threads = K * n > T ? K * n : T;
+    int threads = K * n > T * ((T + 31) / 32) ? K * n : T * ((T + 31) / 32);     // words of the masks are the most to write
     threads = threads >= kPlanMaxThreads ? kPlanMaxThreads : (threads + 31) / 32 * 32;
     SPEC_CUDA_TRY(launch_pdl(tree_plan_kernel, dim3(B), dim3(threads), (size_t)lay.total, (cudaStream_t)cuda_stream, cand_tok,
                              last_tok, seq_len, K, n, T, tok, pos, parent, mask, node_of, n_nodes));
@@ -582,19 +715,23 @@ int spec_verify_tree(const spec_tree_verify_t *v, void *cuda_stream) {
         return SPEC_ERR_SHAPE;
     WalkArgs a;
     a.v = *v;
-    int ctas = 1;
-    while (ctas < kWalkMaxCluster && (long long)ctas * 2048 < v->V) ctas *= 2;
-    a.part = ((v->V + ctas - 1) / ctas + 31) / 32 * 32;
-    const int arrays = (v->hist_tok ? 1 : 0) + (v->bias_tok ? 1 : 0);
-    // as much of the part as 160 KB of tables cover at a time
-    a.pass = a.part;
-    const int cover = 160 * 1024 / (4 * arrays + 1) / 32 * 32;
-    if (arrays && a.pass > cover) a.pass = cover;
-    const size_t smem = arrays ? ((size_t)a.pass * arrays + a.pass / 32) * 4 : 0;
+    // A block per CTA, up to the 8 CTAs that any cluster may have, but no more CTAs than run at the same time (a second round
+    // of clusters costs a whole walk, and fewer CTAs per sequence only some of the rows' latency); 16 where the table does not
+    // fit otherwise.
+    int most = 0, log_ctas = -1;
+    while (most < 3 && ((long long)kBlockTokens << most) < v->V) ++most;
+    size_t smem = 0;
+    for (int l = most; l >= 0; --l) {
+        if (!plan_walk_table(a, l, smem)) continue;
+        log_ctas = l;
+        const size_t per_sm = 227 * 1024 / (smem + 2048);
+        if (((long long)v->B << l) <= (long long)num_sms() * (per_sm < kWalkCtasPerSm ? per_sm : kWalkCtasPerSm)) break;
+    }
+    if (!plan_walk_table(a, log_ctas < 0 ? 4 : log_ctas, smem)) return SPEC_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (v->logits_dtype == SPEC_BF16) return launch_walk<SPEC_BF16>(a, ctas, smem, st);
-    if (v->logits_dtype == SPEC_F16) return launch_walk<SPEC_F16>(a, ctas, smem, st);
-    return launch_walk<SPEC_F32>(a, ctas, smem, st);
+    if (v->logits_dtype == SPEC_BF16) return launch_walk<SPEC_BF16>(a, smem, st);
+    if (v->logits_dtype == SPEC_F16) return launch_walk<SPEC_F16>(a, smem, st);
+    return launch_walk<SPEC_F32>(a, smem, st);
 }
 
 int spec_kv_commit(const spec_kv_commit_t *c, void *cuda_stream) {
@@ -608,6 +745,7 @@ int spec_kv_commit(const spec_kv_commit_t *c, void *cuda_stream) {
         if (c->k_stride[i] % 8 || c->v_stride[i] % 8 || c->kc_stride[i] % 8 || c->vc_stride[i] % 8) return SPEC_ERR_SHAPE;
         if (c->k_stride[i] < 0 || c->v_stride[i] < 0 || c->kc_stride[i] < 0 || c->vc_stride[i] < 0) return SPEC_ERR_INVALID_ARG;
     }
+    if ((long long)c->n_pages * c->page_size > INT_MAX) return SPEC_ERR_SHAPE;
     const long long vecs = 2ll * c->L * c->H * (c->D / 8);
     SPEC_CUDA_TRY(launch_pdl(kv_commit_kernel, dim3((unsigned)((vecs + kCommitThreads - 1) / kCommitThreads), c->B),
                              dim3(kCommitThreads), 0, (cudaStream_t)cuda_stream, *c));

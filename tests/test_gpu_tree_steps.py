@@ -170,7 +170,9 @@ def _constraints(rng, B, T, V, tok, hist_max, bias_max):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("B,K,n,T,V,hist_max,bias_max", [(2, 3, 2, 7, 7, 5, 3), (6, 8, 4, 30, 1000, 300, 20),
-                                                         (3, 16, 3, 40, 32003, 2000, 64), (2, 4, 3, 13, 300007, 900, 30)])
+                                                         (3, 16, 3, 40, 32003, 2000, 64), (2, 4, 3, 13, 300007, 900, 30),
+                                                         (2, 4, 3, 13, 50000, 30000, 5), (1, 4, 3, 13, 262144, 20000, 300),
+                                                         (150, 3, 2, 7, 9000, 40, 3)])
 def test_walk_with_constraints(spec, B, K, n, T, V, hist_max, bias_max, dtype):
     rng = np.random.default_rng(V + hist_max)
     tok, parent, nodes, logits = _walk_case(rng, B, K, n, T, V, dtype)
@@ -187,6 +189,24 @@ def test_walk_with_constraints(spec, B, K, n, T, V, hist_max, bias_max, dtype):
     equal(call(**pick("allow")), ref.walk(tok, parent, nodes, x, n, allow=host["allow"]))
     equal(call(**pick("hist_tok", "hist_len", "repetition")), ref.walk(tok, parent, nodes, x, n, hist=h["hist"], rep=h["rep"]))
     equal(call(**pick("hist_tok", "hist_len", "presence")), ref.walk(tok, parent, nodes, x, n, hist=h["hist"], pres=h["pres"]))
+
+
+def test_equal_tokens_and_many_of_them(spec):
+    """A history of one token, of two in turn, and biases that name one token again and again: the last one counts."""
+    V, H = 70000, 5000
+    tok, parent, nodes = np.array([[3, 60000], [3, 60000]], np.int32), np.array([[-1, 0]] * 2, np.int32), np.array([2, 2], np.int32)
+    logits = np.zeros((2, 2, V), np.float32)
+    logits[:, :, 60000], logits[:, :, 5], logits[:, :, 69999] = 900.0, 500.0, 300.0
+    hist = np.stack([np.full(H, 60000), np.where(np.arange(H) % 2, 60000, 5)]).astype(np.int32)
+    f = np.array([0.125, 0.125], np.float32)
+    bias_tok, bias_val = np.full((2, 600), 69999, np.int32), np.tile(np.arange(600, dtype=np.float32), (2, 1))
+    got = spec.spec_verify_tree(gpu(tok), gpu(parent), gpu(nodes), gpu(logits), n=1, hist_tok=gpu(hist),
+                                hist_len=gpu([H, H], torch.int32), frequency=gpu(f), bias_tok=gpu(bias_tok), bias_val=gpu(bias_val))
+    want = ref.walk(tok, parent, nodes, logits.astype(np.float64), 1, hist=hist.tolist(), freq=f,
+                    bias=[list(zip(a.tolist(), b.tolist())) for a, b in zip(bias_tok, bias_val)])
+    # sequence 0: 900 - 5000 / 8 = 275 < 500; sequence 1: 900 - 312.5 = 587.5, 500 - 312.5; and 300 + 599 = 899 is above them all
+    equal(got, want)
+    assert got[2].tolist() == [69999, 69999]
 
 
 def test_penalties_count_the_tokens_taken_on_the_walk(spec):
@@ -284,3 +304,79 @@ def test_kv_commit_skips_what_is_out_of_range(spec):
     for c in caches:
         assert np.array_equal(c.cpu().numpy().reshape(want.shape), want)
     assert new_len.tolist() == [3] * B and spec.spec_poll_error(err) == spec.SPEC_ERR_INDEX_RANGE
+
+
+# ---- marshalling ---------------------------------------------------------------------------------------------------
+def test_both_ways_of_marshalling_give_the_same(spec, monkeypatch):
+    if spec._pycall is None:
+        pytest.skip("built without the interpreter's headers")
+    rng = np.random.default_rng(3)
+    B, K, n, T, V = 3, 6, 3, 14, 700
+    cand = ref.random_candidates(rng, B, K, n, V)
+    last, lens = rng.integers(0, V, B).astype(np.int32), np.array([7, 0, 300], np.int32)
+    logits = torch.from_numpy(rng.normal(0, 2, (B, T, V))).to(torch.float16).cuda()
+    hist = gpu(rng.integers(0, V, (B, 50)), torch.int32)
+    kv = torch.from_numpy(rng.normal(0, 1, (2, B, T, 3, 2, 64))).to(torch.bfloat16).cuda()
+    q = torch.from_numpy(rng.normal(0, 1, (B, T, 4, 64))).to(torch.bfloat16).cuda()
+
+    def run():
+        words = lambda *s, dtype=torch.int32: torch.zeros(s, dtype=dtype, device="cuda")
+        tree = spec.SpecTree(words(B, T), words(B, T), words(B, T), words(B, T, 1), words(B, K, n + 1), words(B))
+        spec.spec_tree_plan(gpu(cand), gpu(last), gpu(lens), T, tree=tree)
+        table, held, count = words(B, 30), words(B), gpu([90], torch.int32)
+        slots = words(B, n + 1, dtype=torch.int64)
+        free = torch.arange(90, dtype=torch.int32, device="cuda")
+        spec.spec_page_tables(gpu(lens), None, table, held, free, count, 16, slots=slots)
+        caches = torch.ones(2, 2, 90, 16, 2, 64, dtype=torch.bfloat16, device="cuda")
+        out, lse = torch.zeros_like(q), torch.zeros(B, T, 4, device="cuda")
+        ws = words(spec.spec_tree_attention_workspace_bytes(B, T, 4, 2, 64), dtype=torch.uint8)
+        spec.spec_tree_attention(q, kv[0, :, :, 0], kv[0, :, :, 1], caches[0, 0], caches[1, 0], table, gpu(lens), mask=tree.mask,
+                                 n_nodes=tree.n_nodes, out=out, lse=lse, workspace=ws)
+        outs = words(B), words(B), words(B), words(B, n + 1)
+        spec.spec_verify_tree(tree.tok, tree.parent, tree.n_nodes, logits, hist_tok=hist, hist_len=gpu([50, 3, 0], torch.int32),
+                              frequency=gpu([0.5, 0.1, 0.2], torch.float32), accept_len=outs[0], last_node=outs[1],
+                              next_tok=outs[2], path=outs[3])
+        new_len = words(B)
+        spec.spec_kv_commit(kv[..., 1, :, :], kv[..., 2, :, :], caches[0], caches[1], outs[3], outs[0], slots, gpu(lens),
+                            new_len=new_len)
+        return (*tree, table, held, count, slots, out, lse, *outs, caches, new_len)
+
+    calls = []
+    for name in ("tree_plan", "page_tables", "tree_attention", "verify_tree", "kv_commit"):
+        real = getattr(spec._pycall, name)
+        monkeypatch.setattr(spec._pycall, name, lambda *a, _r=real, _n=name: calls.append((_n, _r(*a))) or calls[-1][1])
+    fast = run()
+    assert [c[0] for c in calls] == ["tree_plan", "page_tables", "tree_attention", "verify_tree", "kv_commit"]
+    assert all(status == spec.SPEC_OK for _, status in calls)
+    monkeypatch.setattr(spec, "_pycall", None)
+    for a, b in zip(fast, run()):
+        assert torch.equal(a, b)
+
+
+def test_marshalling_leaves_what_is_wrong_to_the_checks(spec):
+    z = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt, device="cuda")
+    h = torch.bfloat16
+    tree = spec.SpecTree(z(1, 4), z(1, 4), z(1, 4), z(1, 4, 1), z(1, 2, 4), z(1))
+    good = (z(1, 2, 3), z(1), z(1), 4)
+    spec.spec_tree_plan(*good, tree=tree)
+    for bad in (tree._replace(tok=z(1, 5)), tree._replace(mask=z(1, 4)), tree._replace(n_nodes=z(1).cpu()),
+                tree._replace(parent=z(4, 1).T[:, ::1].expand(1, 4)[:, [0, 1, 2, 3]].long())):
+        with pytest.raises(ValueError):
+            spec.spec_tree_plan(*good, tree=bad)
+    for slots in (z(1, 3), z(2, 3, dt=torch.int64)):
+        with pytest.raises(ValueError):
+            spec.spec_page_tables(z(1), None, z(1, 4), z(1), z(8), z(1), 16, slots=slots)
+    with pytest.raises(ValueError):
+        spec.spec_page_tables(z(2), None, z(1, 4).expand(2, 4), z(2), z(8), z(1), 16, slots=z(2, 3, dt=torch.int64))
+    outs = dict(accept_len=z(1), last_node=z(1), next_tok=z(1), path=z(1, 3))
+    for bad in (dict(logits=z(1, 4, 9)), dict(hist_tok=z(2, 3)), dict(allow=z(1, 4, 2)), dict(bias_tok=z(1, 3)),
+                dict(repetition=z(1)), dict(path=z(2, 3))):
+        args = {**dict(tok=z(1, 4), parent=z(1, 4), n_nodes=z(1), logits=z(1, 4, 9, dt=h)), **outs, **bad}
+        with pytest.raises((ValueError, spec.SpecError)):
+            spec.spec_verify_tree(**args)
+    kv, cache = z(1, 1, 4, 2, 64, dt=h), z(1, 3, 16, 2, 64, dt=h)
+    for bad in (dict(path=z(1, 3).long()), dict(slots=z(1, 3)), dict(k_cache=cache[..., :32]),
+                dict(v_cache=cache[:, :1].expand(1, 3, 16, 2, 64)), dict(v=kv.float())):
+        args = {**dict(k=kv, v=kv, k_cache=cache, v_cache=cache, path=z(1, 3), accept_len=z(1), slots=z(1, 3, dt=torch.int64)), **bad}
+        with pytest.raises(ValueError):
+            spec.spec_kv_commit(**args)

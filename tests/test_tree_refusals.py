@@ -100,6 +100,10 @@ def test_verify_tree(b):
     assert b._lib.spec_verify_tree(None, None) == b.SPEC_ERR_INVALID_ARG
 
 
+def test_constraints_that_fit_no_table(b):
+    assert _verify(b, V=1 << 22, max_hist=1 << 20) == b.SPEC_ERR_SHAPE
+
+
 def _commit(b, **bad):
     f = dict(L=3, B=2, T=5, n=3, H=2, D=64, page=16, pages=9, ptrs=[P] * 4, path=P, accept=P, slots=P, lens=P, new=P, err=0,
              strides=[64] * 16)
@@ -117,7 +121,7 @@ def test_kv_commit(b):
         dict(page=0), dict(pages=0), dict(strides=[-64] + [64] * 15)]
     for bad in invalid:
         assert _commit(b, **bad) == b.SPEC_ERR_INVALID_ARG, bad
-    for bad in (dict(D=60), dict(B=65536), dict(strides=[64] * 15 + [60])):
+    for bad in (dict(D=60), dict(B=65536), dict(strides=[64] * 15 + [60]), dict(pages=1 << 28)):
         assert _commit(b, **bad) == b.SPEC_ERR_SHAPE, bad
     assert b._lib.spec_kv_commit(None, None) == b.SPEC_ERR_INVALID_ARG
 
