@@ -248,14 +248,14 @@ __global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(const TableArg
 // ---- the greedy walk -----------------------------------------------------------------------------------------------
 // A cluster of CTAs per sequence; the vocabulary goes to them in blocks of 4096 tokens in turn.  Per step every CTA finds the
 // maximum of its blocks of the current node's row, the CTAs exchange theirs through distributed shared memory, and all of them
-// look up the child that carries the winner.  Only the rows on the path are read, so a step is latency: loads of four vectors
-// per thread in flight, one exchange, one look at the tree, which lies in shared memory.
+// look up the child that carries the winner.  Only the rows on the path are read, so a step is latency: the loads of a row (1.5 us
+// at a vocabulary of 32000), one exchange (1 us), one look at the tree, which lies in shared memory (0.5 us).
 //
 // Constraints.  The tokens that penalties or biases touch are few.  Each CTA counts those of its blocks once, in a table in
 // shared memory, and marks them in a bitmap: the pass over the row leaves them out (and what the grammar forbids), and every
 // listed token is looked at by itself.  The table is hashed while that is smaller, which lets four CTAs share an SM for
-// histories of a few thousand tokens (64 sequences of a vocabulary of 128256, histories of up to 2048: 278 us with a dense table of
-// 130 KB and per-element checks), else it has an entry per token.
+// histories of a few thousand tokens, else it has an entry per token.  64 sequences, a vocabulary of 128256, histories of up to
+// 2048 tokens, a grammar: 63 us (34 without constraints); a table of 130 KB and checks per element took 278.
 constexpr int kWalkThreads = 256;
 constexpr int kWalkWarps = kWalkThreads / 32;
 constexpr int kWalkCtasPerSm = 4;            // by registers
@@ -268,7 +268,7 @@ constexpr uint32_t kFree = 0xffffffffu;      // of a key
 struct WalkArgs {
     spec_tree_verify_t v;
     int log_ctas;
-    int cap;                                 // entries of the table: a power of two (hashed) or the CTA's tokens; 0: no constraints by token
+    int cap;                                 // entries of the table: somewhat more than max_list (hashed) or the CTA's tokens; 0: no constraints by token
     int hashed, max_list, part;              // part: tokens of a CTA, whole blocks
 };
 
@@ -297,6 +297,14 @@ template <> struct Logit<SPEC_BF16> {
         return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
     }
     static __device__ __forceinline__ float at(const void *row, int i) { return bf16_bits_to_float(((const uint16_t *)row)[i]); }
+    // the greatest of a vector; NaN only if all are
+    static __device__ __forceinline__ float most(const uint4 &v) {
+        uint32_t a, b;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+        return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    }
 };
 template <> struct Logit<SPEC_F16> {
     static constexpr int kBytes = 2;
@@ -307,11 +315,22 @@ template <> struct Logit<SPEC_F16> {
     static __device__ __forceinline__ float at(const void *row, int i) {
         return __half2float(__ushort_as_half(((const unsigned short *)row)[i]));
     }
+    static __device__ __forceinline__ float most(const uint4 &v) {
+        uint32_t a, b;
+        asm("max.f16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.f16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.f16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+        const __half2 h = *(__half2 *)&a;
+        return fmaxf(__low2float(h), __high2float(h));
+    }
 };
 template <> struct Logit<SPEC_F32> {
     static constexpr int kBytes = 4;
     static __device__ __forceinline__ float get(const uint4 &v, int i) { return __uint_as_float((&v.x)[i]); }
     static __device__ __forceinline__ float at(const void *row, int i) { return ((const float *)row)[i]; }
+    static __device__ __forceinline__ float most(const uint4 &v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
 };
 
 struct Best {
@@ -357,11 +376,11 @@ __device__ __forceinline__ int table_entry(const WalkArgs &a, const WalkTable &w
     const int local = local_token(a, t);
     int at = local;
     if (a.hashed) {
-        at = (int)((uint32_t)t * 0x9e3779b1u >> 8) & (a.cap - 1);
+        at = (int)__umulhi((uint32_t)t * 0x9e3779b1u, (uint32_t)a.cap);
         for (;;) {                                       // there are fewer tokens than entries
             const uint32_t was = atomicCAS(&w.key[at], kFree, (uint32_t)t);
             if (was == kFree || was == (uint32_t)t) break;
-            at = (at + 1) & (a.cap - 1);
+            at = at + 1 == a.cap ? 0 : at + 1;
         }
     }
     const uint32_t bit = 1u << (local & 31);
@@ -382,65 +401,110 @@ __device__ __forceinline__ float walk_adjust(const WalkArgs &a, const WalkTable 
     return x;
 }
 
-// Bits of n <= 8 consecutive positions of a bit field, from `first` on.
-__device__ __forceinline__ uint32_t bits_from(const uint32_t *field, int first, int words) {
-    const int w = first >> 5;
-    return __funnelshift_r(field[w], w + 1 < words ? field[w + 1] : 0u, first & 31);
+// Eight consecutive bits of a bit field of `bytes` bytes, from `first` on.
+__device__ __forceinline__ uint32_t bits_from(const uint32_t *field, int first, int bytes) {
+    const uint8_t *p = (const uint8_t *)field;
+    uint32_t x = p[first >> 3];
+    if (first & 7) {
+        if ((first >> 3) + 1 < bytes) x |= (uint32_t)p[(first >> 3) + 1] << 8;
+        x >>= first & 7;
+    }
+    return x & 0xffu;
 }
 
-// Elements [begin, end) of a row: those that `allow` (null: all) and not `skip` (null: none; bits of the elements from skip0 on) leave.
+// A vector with what `use` does not keep at minus infinity.
 template <int kDtype>
-__device__ __forceinline__ void scan_block(const char *row, int V, int begin, int end, const uint32_t *allow, int words,
-                                           const uint32_t *skip, int skip0, int skip_words, Best &best) {
-    constexpr int kPer = 16 / Logit<kDtype>::kBytes, kUnroll = 4;
-    const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);       // elements behind a vector's start
-    const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
-    const int v0 = (begin + skew) / kPer, v1 = (end + skew + kPer - 1) / kPer;
-    for (int i0 = v0 + threadIdx.x; i0 < v1; i0 += kWalkThreads * kUnroll) {
-        uint4 x[kUnroll];
-        uint32_t use[kUnroll];
+__device__ __forceinline__ void blank(uint4 &x, uint32_t use) {
+    constexpr uint32_t kNone = kDtype == SPEC_BF16 ? 0xff80ff80u : 0xfc00fc00u;
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const int i = i0 + k * kWalkThreads, e0 = i * kPer - skew;
-            use[k] = 0;
-            if (i >= v1) continue;
-            // a vector that reaches beyond the row is read element by element: the memory there may be nobody's
-            if (e0 >= 0 && e0 + kPer <= V) {
-                x[k] = __ldg(vec + i);
-            } else {
-                uint32_t y[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    if (e0 + e < 0 || e0 + e >= V) continue;
-                    if (Logit<kDtype>::kBytes == 2) y[e / 2] |= (uint32_t)((const uint16_t *)row)[e0 + e] << 16 * (e % 2);
-                    else y[e] = ((const uint32_t *)row)[e0 + e];
-                }
-                x[k] = make_uint4(y[0], y[1], y[2], y[3]);
-            }
-            uint32_t m = (1u << kPer) - 1;
-            if (e0 < begin) m &= m << (begin - e0);
-            if (e0 + kPer > end) m &= (1u << kPer) - 1 >> (e0 + kPer - end);
-            const int from = max(e0, begin), shift = from - e0;
-            if (allow != nullptr) m &= bits_from(allow, from, words) << shift;
-            if (skip != nullptr) m &= ~(bits_from(skip, from - skip0, skip_words) << shift);
-            use[k] = m;
-        }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const int e0 = (i0 + k * kWalkThreads) * kPer - skew;
-            if (use[k] == 0) continue;
-            float top = -INFINITY;
-            int pos = 0;
-#pragma unroll
-            for (int e = kPer - 1; e >= 0; --e) {        // downwards: of equal ones the first stays
-                const float y = fmaxf(Logit<kDtype>::get(x[k], e), -INFINITY);       // (a NaN counts as minus infinity)
-                const bool take = (use[k] >> e & 1) && y >= top;
-                top = take ? y : top;
-                pos = take ? e : pos;
-            }
-            best.offer(top, e0 + pos);
+    for (int i = 0; i < 4; ++i) {
+        uint32_t &w = (&x.x)[i];
+        if (kDtype == SPEC_F32) {
+            if (!(use >> i & 1)) w = 0xff800000u;
+        } else {
+            const uint32_t keep = (use >> 2 * i & 1) * 0xffffu | (use >> (2 * i + 1) & 1) * 0xffff0000u;
+            w = (w & keep) | (kNone & ~keep);
         }
     }
+}
+
+// The maximum over this CTA's blocks of a row, of the tokens that `allow` (null: all) and `marked` (null: none) leave.  A thread's
+// vectors rise and four of them (and the grammar's bits) are in flight.  It keeps the vector with the greatest maximum, without a
+// branch, and looks for the element at the end: a branch for every new maximum is taken by some lane nearly always.
+template <int kDtype>
+__device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uint32_t rank, const uint32_t *allow, int words,
+                                         const uint32_t *marked, Best &best) {
+    constexpr int kPer = 16 / Logit<kDtype>::kBytes, kPerThread = kBlockTokens / kPer / kWalkThreads, kAhead = 4;
+    constexpr uint32_t kAll = (1u << kPer) - 1;
+    const int V = a.v.V;
+    const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);       // elements behind a vector's start
+    const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
+    const int blocks = (V + kBlockTokens - 1) / kBlockTokens;
+    const int turns = (blocks - (int)rank + (1 << a.log_ctas) - 1) >> a.log_ctas;
+    uint4 best_x = make_uint4(0, 0, 0, 0);
+    float best_top = -INFINITY;
+    uint32_t best_use = 0;
+    int best_e0 = 0;
+    auto first_of = [&](int turn) { return ((turn << a.log_ctas) + (int)rank) * kBlockTokens; };
+    auto look = [&](uint4 x, int e0, int begin, int turn, uint32_t use) {        // use: the grammar's bits from max(e0, begin) on
+        const int from = max(e0, begin);
+        use = use << (from - e0) & kAll;
+        if (e0 + kPer > begin + kBlockTokens) use &= kAll >> (e0 + kPer - begin - kBlockTokens);
+        if (e0 + kPer > V) use &= kAll >> (e0 + kPer - V);
+        if (marked != nullptr) use &= ~(bits_from(marked, turn * kBlockTokens + from - begin, a.part / 8) << (from - e0));
+        if (e0 < 0 || e0 + kPer > V) {                   // a vector that reaches beyond the row: the memory there may be nobody's
+            uint32_t y[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                if (e0 + e < 0 || e0 + e >= V) continue;
+                if (Logit<kDtype>::kBytes == 2) y[e / 2] |= (uint32_t)((const uint16_t *)row)[e0 + e] << 16 * (e % 2);
+                else y[e] = ((const uint32_t *)row)[e0 + e];
+            }
+            x = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        if (use != kAll) blank<kDtype>(x, use);
+        const float top = fmaxf(Logit<kDtype>::most(x), -INFINITY);
+        const bool take = use != 0 && (best_use == 0 || top > best_top);
+        best_top = take ? top : best_top;
+        best_use = take ? use : best_use;
+        best_e0 = take ? e0 : best_e0;
+        best_x.x = take ? x.x : best_x.x;
+        best_x.y = take ? x.y : best_x.y;
+        best_x.z = take ? x.z : best_x.z;
+        best_x.w = take ? x.w : best_x.w;
+    };
+    for (int turn0 = 0; turn0 < turns; turn0 += kAhead / kPerThread) {
+        uint4 x[kAhead];
+        uint32_t use[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int turn = turn0 + k / kPerThread, begin = first_of(turn);
+            const int e0 = begin - skew + ((int)threadIdx.x + k % kPerThread * kWalkThreads) * kPer;
+            use[k] = kAll;
+            x[k] = make_uint4(0, 0, 0, 0);
+            if (turn >= turns || e0 >= V) continue;
+            if (e0 >= 0 && e0 + kPer <= V) x[k] = __ldg((const uint4 *)((const char *)vec + (long long)(e0 + skew) * Logit<kDtype>::kBytes));
+            if (allow != nullptr) use[k] = bits_from(allow, max(e0, begin), words * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int turn = turn0 + k / kPerThread, begin = first_of(turn);
+            const int e0 = begin - skew + ((int)threadIdx.x + k % kPerThread * kWalkThreads) * kPer;
+            if (turn < turns && e0 < V) look(x[k], e0, begin, turn, use[k]);
+        }
+    }
+    if (skew)                                            // the vectors in which blocks end
+        for (int turn = threadIdx.x; turn < turns; turn += kWalkThreads) {
+            const int begin = first_of(turn), e0 = begin - skew + kBlockTokens;
+            if (e0 >= V) continue;
+            const uint4 x = e0 + kPer <= V ? __ldg((const uint4 *)((const char *)vec + (long long)(e0 + skew) * Logit<kDtype>::kBytes))
+                                           : make_uint4(0, 0, 0, 0);
+            look(x, e0, begin, turn, allow != nullptr ? bits_from(allow, e0, words * 4) : kAll);
+        }
+    if (best_use == 0) return;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)                       // (a NaN counts as minus infinity)
+        if (best_use >> e & 1) best.offer(Logit<kDtype>::get(best_x, e), best_e0 + e);
 }
 
 template <int kDtype>
@@ -484,16 +548,25 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
         if (v.hist_tok != nullptr) {
             const int size = min(v.hist_len[b], v.max_hist), prompt = v.prompt_len == nullptr ? 0 : v.prompt_len[b];
             const int32_t *hist = v.hist_tok + (size_t)b * v.max_hist;
-            for (int i0 = 0; i0 < size; i0 += kWalkThreads) {
-                const int i = i0 + t, h = i < size ? hist[i] : -1;
-                const bool mine = i < size && owns(a, rank, h);
-                // equal tokens of a warp are counted together: a few tokens make up most of a text
-                const unsigned same = __match_any_sync(0xffffffffu, mine ? h : -1);
-                const unsigned made = __ballot_sync(0xffffffffu, mine && i >= prompt) & same;
-                if (mine && lane == __ffs(same) - 1) {
-                    const int at = table_entry(a, w, h);
-                    atomicOr(&w.count[at], kSeen);
-                    if (made) atomicAdd(&w.count[at], (uint32_t)__popc(made));
+            constexpr int kAhead = 2;
+            for (int i0 = 0; i0 < size; i0 += kWalkThreads * kAhead) {
+                int h[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const int i = i0 + k * kWalkThreads + t;
+                    h[k] = i < size ? hist[i] : -1;
+                    if (!owns(a, rank, h[k])) h[k] = -1;
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    // equal tokens of a warp are counted together: a few tokens make up most of a text
+                    const unsigned same = __match_any_sync(0xffffffffu, h[k]);
+                    const unsigned made = __ballot_sync(0xffffffffu, i0 + k * kWalkThreads + t >= prompt) & same;
+                    if (h[k] >= 0 && lane == __ffs(same) - 1) {
+                        const int at = table_entry(a, w, h[k]);
+                        atomicOr(&w.count[at], kSeen);
+                        if (made) atomicAdd(&w.count[at], (uint32_t)__popc(made));
+                    }
                 }
             }
         }
@@ -514,9 +587,7 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
             const char *row = (const char *)v.logits + ((long long)b * v.logits_stride[0] + (long long)cur * v.logits_stride[1]) *
                                                            Logit<kDtype>::kBytes;
             const uint32_t *allow = v.allow == nullptr ? nullptr : v.allow + ((size_t)b * v.T + cur) * words;
-            for (int block = rank, local = 0; block * kBlockTokens < V; block += ranks, local += kBlockTokens)
-                scan_block<kDtype>(row, V, block * kBlockTokens, min((block + 1) * kBlockTokens, V), allow, words,
-                                   a.cap ? w.marked : nullptr, block * kBlockTokens - local, a.part / 32, best);
+            scan_row<kDtype>(a, row, rank, allow, words, a.cap ? w.marked : nullptr, best);
             if (a.cap) {
                 const int n = n_list;
                 for (int i = t; i < n; i += kWalkThreads) {
@@ -639,8 +710,7 @@ bool plan_walk_table(WalkArgs &a, int log_ctas, size_t &smem) {
     if (!per_entry) return true;
     const long long tokens = (long long)v.max_hist + v.max_bias + v.n;
     const long long listed = tokens < part ? tokens : part;
-    long long cap = 256;
-    while (cap * 3 < listed * 4) cap *= 2;               // three quarters full at most
+    long long cap = listed + listed / 3 + 8;             // three quarters full at most
     const bool hashed = cap * (per_entry + 4) < part * per_entry;
     if (!hashed) cap = part;
     smem = tree + (size_t)cap * (per_entry + (hashed ? 4 : 0)) + (size_t)part / 8 + (size_t)listed * 4;
@@ -724,8 +794,8 @@ int spec_verify_tree(const spec_tree_verify_t *v, void *cuda_stream) {
     for (int l = most; l >= 0; --l) {
         if (!plan_walk_table(a, l, smem)) continue;
         log_ctas = l;
-        const size_t per_sm = 227 * 1024 / (smem + 2048);
-        if (((long long)v->B << l) <= (long long)num_sms() * (per_sm < kWalkCtasPerSm ? per_sm : kWalkCtasPerSm)) break;
+        const long long per_sm = 227 * 1024 / ((long long)smem + 2048);
+        if (((long long)v->B << l) <= num_sms() * (per_sm < kWalkCtasPerSm ? per_sm : kWalkCtasPerSm)) break;
     }
     if (!plan_walk_table(a, log_ctas < 0 ? 4 : log_ctas, smem)) return SPEC_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;

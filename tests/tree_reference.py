@@ -1,6 +1,7 @@
 """Plain implementations, in 64 bits and on the host, of the operators around the base model's forward pass over a tree of drafted
 tokens, and the inputs that their tests share."""
 import math
+from collections import Counter
 
 import numpy as np
 import torch
@@ -158,8 +159,8 @@ def walk(tok, parent, nodes, logits, n, hist=None, prompt=None, rep=None, freq=N
                 for t in set(text + went):
                     r = 1.0 if rep is None else float(rep[b])
                     x[t] = x[t] / r if x[t] > 0 else x[t] * r
-                for t in set(written):
-                    x[t] -= (0.0 if freq is None else float(freq[b])) * written.count(t)
+                for t, times in Counter(written).items():
+                    x[t] -= (0.0 if freq is None else float(freq[b])) * times
                     x[t] -= 0.0 if pres is None else float(pres[b])
             if bias is not None:
                 for t, value in {t: value for t, value in bias[b] if 0 <= t < V}.items():
