@@ -637,10 +637,10 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
 }
 
 // ---- accepted keys and values --------------------------------------------------------------------------------------
-// A thread copies 16 bytes of every accepted row, the loads of eight rows in flight before the first store: bound by HBM
-// for batches, by latency for few sequences.
+// A thread copies 16 bytes of every accepted row, the loads of two rows in flight before the first store (more cost occupancy:
+// 13.2 us with two, 14.3 with six, 15.9 with eight at 50 MB): bound by HBM for batches, by latency for few sequences.
 constexpr int kCommitThreads = 256;
-constexpr int kCommitRows = 8;
+constexpr int kCommitRows = 2;
 
 __device__ __forceinline__ uint4 ld_once(const uint4 *p) {
     uint4 v;
