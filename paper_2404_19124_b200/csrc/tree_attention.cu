@@ -15,8 +15,10 @@
 //   warps 12-15     bring the others row by row with 16-byte asynchronous copies (rows that do not exist read as zeros): Q, the tile
 //                   in which the cache ends and the tree begins, the tree, and caches whose pages do not tile 128 keys
 // Tiles are 128-byte-swizzled either way.
-// Two streams keep the tensor cores busy while a softmax runs.  Units of more than 128 rows have a stream per 128 rows, both on the
-// same tile of keys; smaller ones give their tiles to the streams in turn, and the two results are joined at the end.
+// Two streams of softmax, 64 keys at a step, each with two score buffers, so that the scores of the next step are there when one
+// is done and the products of the last step run meanwhile.  (With one buffer of 128 keys per stream neither the tensor cores, 43 %
+// busy, nor the exponentials, 39 %, were the limit, but the way round.)  Units of more than 128 rows have a stream per 128
+// rows, which take both halves of every tile of keys; in smaller ones each stream takes a half, and the two results are joined.
 #include <limits.h>
 #include <math.h>
 
@@ -40,6 +42,7 @@ using tc::umma_commit;
 
 constexpr int kTileKeys = 128;
 constexpr int kTileRows = 128;
+constexpr int kStepKeys = 64;
 constexpr int kHalfBytes = kTileKeys * 128;     // 64 columns of a tile of 128 rows
 constexpr int kSoftmaxThreads = 256;
 constexpr int kBoxWarps = 3;
@@ -55,7 +58,7 @@ constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns e
 constexpr int kUnitFlags = 8;
 constexpr uint64_t kWaitMaxNs = 1000000000;     // after which a wait gives up
 constexpr uint32_t kWaitHintNs = 20000;
-constexpr float kRescaleAbove = 8.f;            // see softmax_tile
+constexpr float kRescaleAbove = 8.f;            // see softmax_step
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -87,7 +90,7 @@ struct Deal {
 
 struct Shared {
     uint64_t q_full[2], q_empty[2], k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
-    uint64_t s_full[2], p_full[2], pv_done[2], meet, drained, boxes_asked, rows_asked;
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], meet, drained, boxes_asked, rows_asked;
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see load_v)
@@ -575,14 +578,15 @@ __device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32
     const uint32_t tmem = sh->tmem_base;
     const int k_steps = (g.a.D + 15) / 16;
     int qs = 0, ks = 0, vs = 0;
-    uint32_t qp = 0, kp = 0, vp = 0, pp[2] = {0, 0};
+    uint32_t qp = 0, kp = 0, vp = 0;
+    uint32_t count = 0;                                  // steps of either stream in the units before
     Walk walk(g, sh);
     Unit u;
     while (walk.next(g, u)) {
+        // step j: stream j & 1, its buffer by its own count.  two: tile j / 4, half (j / 2) & 1; else tile j / 2, half j & 1
         const bool two = u.two_tiles();
-        const int steps = (u.t1 - u.t0) * (two ? 2 : 1);
-        // slots of the unit's query tiles
-        const int q0 = qs, q1 = two ? qs ^ 1 : qs;
+        const int steps = (u.t1 - u.t0) * (two ? 4 : 2);
+        const int q0 = qs, q1 = two ? qs ^ 1 : qs;       // slots of the unit's query tiles
         const uint32_t qp0 = qp, qp1 = two && qs == 1 ? qp ^ 1 : qp;
         if (!two) {
             if (++qs == R::kQ) qs = 0, qp ^= 1;
@@ -590,47 +594,50 @@ __device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32
             qp ^= 1;
         }
         auto scores = [&](int j) -> bool {
-            const int s = j & 1, q = s ? q1 : q0;
+            const int s = j & 1, half = two ? j >> 1 & 1 : s, q = s ? q1 : q0;
+            const uint32_t buf = (count + (j >> 1)) & 1;
             if (j < 2 && !wait(&sh->q_full[q], s ? qp1 : qp0, sh, err)) return false;
             if (!wait(&sh->k_full[ks], kp, sh, err)) return false;
             fence_async_proxy();
             // (Unrolled, with descriptors that differ by constants: a loop that builds them took 140 cycles an MMA, twice its time.)
-            const uint64_t qd = tc::make_smem_desc(q_tiles + q * R::kBytes), kd = tc::make_smem_desc(k_tiles + ks * R::kBytes);
-            const uint32_t d = tmem + s * 128, desc = g.desc_qk;
+            const uint64_t qd = tc::make_smem_desc(q_tiles + q * R::kBytes);
+            const uint64_t kd = tc::make_smem_desc(k_tiles + ks * R::kBytes + half * kStepKeys * 128);
+            const uint32_t d = tmem + s * 128 + buf * 64, desc = g.desc_qk;
 #pragma unroll
             for (int i = 0; i < 4 * kHalves; ++i) {
                 constexpr int kHalf = kHalfBytes >> 4;
                 const int off = (i >> 2) * kHalf + (i & 3) * 2;
                 if (i < k_steps) mma_ss(d, qd + off, kd + off, desc, i > 0);
             }
-            umma_commit(&sh->s_full[s]);
-            if (!two || s) {
+            umma_commit(&sh->s_full[s][buf]);
+            if (s && (!two || half)) {
                 umma_commit(&sh->k_empty[ks]);
                 if (++ks == R::kK) ks = 0, kp ^= 1;
             }
-            if (j >= steps - (two ? 2 : 1)) umma_commit(&sh->q_empty[q]);
+            if (j == steps - 1 || (two && j == steps - 2)) umma_commit(&sh->q_empty[q]);
             return true;
         };
-        for (int j = 0; j < 2 && j < steps; ++j)
+        for (int j = 0; j < 4 && j < steps; ++j)
             if (!scores(j)) return false;
         for (int j = 0; j < steps; ++j) {
-            const int s = j & 1;
-            if (!wait(&sh->p_full[s], pp[s], sh, err)) return false;
-            pp[s] ^= 1;
+            const int s = j & 1, half = two ? j >> 1 & 1 : s;
+            const uint32_t at = count + (j >> 1), buf = at & 1;
+            if (!wait(&sh->p_full[s][buf], at >> 1 & 1, sh, err)) return false;
             if (!wait(&sh->v_full[vs], vp, sh, err)) return false;
             fence_async_proxy();
             tc_fence_after();
-            const uint64_t vd = v_desc(v_tiles + vs * R::kBytes);
-            const uint32_t d = tmem + 256 + s * 128, pa = tmem + s * 128, desc = g.desc_pv;
+            const uint64_t vd = v_desc(v_tiles + vs * R::kBytes + half * kStepKeys * 128);
+            const uint32_t d = tmem + 256 + s * 128, pa = tmem + s * 128 + buf * 64, desc = g.desc_pv;
 #pragma unroll
-            for (int i = 0; i < kTileKeys / 16; ++i) mma_ts(d, pa + i * 8, vd + i * (2048 >> 4), desc, j >= 2 || i > 0);
-            umma_commit(&sh->pv_done[s]);
-            if (!two || s) {
+            for (int i = 0; i < kStepKeys / 16; ++i) mma_ts(d, pa + i * 8, vd + i * (2048 >> 4), desc, j >= 2 || i > 0);
+            umma_commit(&sh->pv_done[s][buf]);
+            if (s && (!two || half)) {
                 umma_commit(&sh->v_empty[vs]);
                 if (++vs == R::kV) vs = 0, vp ^= 1;
             }
-            if (j + 2 < steps && !scores(j + 2)) return false;
+            if (j + 4 < steps && !scores(j + 4)) return false;
         }
+        count += steps / 2;
     }
     return true;
 }
@@ -677,7 +684,7 @@ struct Row {
     float sum;
 };
 
-__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[128], int at) {
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v, int at) {
 #define V(i) "=f"(v[at + i])
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -689,17 +696,13 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[128],
 #undef V
 }
 // Nothing may use a register before the wait, so each passes through a statement behind it.
-__device__ __forceinline__ void tmem_ld_wait(float (&v)[128]) {
+template <int kN>
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[kN]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int c = 0; c < 128; c += 8)
+    for (int c = 0; c < kN; c += 8)
         asm volatile("" : "+f"(v[c]), "+f"(v[c + 1]), "+f"(v[c + 2]), "+f"(v[c + 3]), "+f"(v[c + 4]), "+f"(v[c + 5]), "+f"(v[c + 6]),
                           "+f"(v[c + 7]));
-}
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
-#pragma unroll
-    for (int c = 0; c < 128; c += 32) tmem_ld32_async(taddr + c, v, c);
-    tmem_ld_wait(v);
 }
 
 // Two lanes of fp32 arithmetic in one instruction.
@@ -716,22 +719,24 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return *(float2 *)&r;
 }
 
-// One tile of a row: probabilities in place of the scores.  The maximum follows the tiles lazily: probabilities are taken against an
+// One step of a row: probabilities in place of the scores.  The maximum follows the steps lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
-// saves nearly every pass over the accumulated output (a pass waits for the products of the tile before).
+// saves nearly every pass over the accumulated output (a pass waits for the products of the step before).
 template <int kDtype, int kHalves>
-__device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
-                                             uint64_t *pv_done, uint32_t pv_parity, bool masked, const uint32_t (&seen)[4], Row &row) {
-    float x[128];
-    tmem_ld128(s_addr, x);
+__device__ __forceinline__ bool softmax_step(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
+                                             uint64_t *pv_done, uint32_t pv_parity, bool masked, uint64_t seen, Row &row) {
+    float x[kStepKeys];
+    tmem_ld32_async(s_addr, x, 0);
+    tmem_ld32_async(s_addr + 32, x, 32);
+    tmem_ld_wait(x);
     if (masked) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-            if (!(seen[i >> 5] >> (i & 31) & 1)) x[i] = -INFINITY;
+        for (int i = 0; i < kStepKeys; ++i)
+            if (!(seen >> i & 1)) x[i] = -INFINITY;
     }
     float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < 128; i += 2) top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
+    for (int i = 0; i < kStepKeys; i += 2) top4[i / 2 % 4] = fmaxf(fmaxf(x[i], x[i + 1]), top4[i / 2 % 4]);
     float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
     top = top == -INFINITY ? top : top * g.scale_log2;
     float shrink = 1.f;
@@ -759,7 +764,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnArgs &g, Shared *sh, uint
     const float2 scale = make_float2(g.scale_log2, g.scale_log2), minus = make_float2(-base, -base);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < kStepKeys / 32; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
@@ -810,8 +815,7 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
     const spec_tree_attention_t &a = g.a;
     const int stream = threadIdx.x >> 7, lane_row = threadIdx.x & 127;
     const uint32_t lanes = sh->tmem_base + ((uint32_t)(lane_row & ~31) << 16);
-    const uint32_t s_addr = lanes + stream * 128;
-    uint32_t steps_done = 0, meet = 0;                   // steps of this stream over all units; parity
+    uint32_t count = 0, meet = 0;                        // steps of this stream over all units; parity
     Walk walk(g, sh);
     Unit u;
     while (walk.next(g, u)) {
@@ -823,28 +827,24 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
         const RowMask mask = {a.mask == nullptr ? nullptr : a.mask + ((size_t)u.b * a.T + node) * n_words, n_words, u.nodes, node};
         Row row = {-INFINITY, 0.f};
         bool first = true;
-        for (int t = two ? u.t0 : u.t0 + stream; t < u.t1; t += two ? 1 : 2) {
-            const int key0 = t * kTileKeys - u.len;
-            const bool masked = key0 + kTileKeys > 0;
-            uint32_t seen[4];
-            if (masked) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) seen[c] = mask.bits(key0 + c * 32);
-            }
-            if (!warp_wait(&sh->s_full[stream], steps_done & 1, sh, a.err_word)) return false;
+        for (int key = u.t0 * kTileKeys + (two ? 0 : stream * kStepKeys); key < u.t1 * kTileKeys; key += two ? kStepKeys : kTileKeys) {
+            const uint32_t buf = count & 1;
+            const int key0 = key - u.len;
+            const bool masked = key0 + kStepKeys > 0;
+            uint64_t seen = 0;
+            if (masked) seen = (uint64_t)mask.bits(key0 + 32) << 32 | mask.bits(key0);
+            if (!warp_wait(&sh->s_full[stream][buf], count >> 1 & 1, sh, a.err_word)) return false;
             tc_fence_after();
-            if (active) {
-                const uint32_t o_addr = lanes + 256 + stream * 128, parity = (steps_done - 1) & 1;
-                const bool ok = softmax_tile<kDtype, kHalves>(g, sh, s_addr, o_addr, first, &sh->pv_done[stream], parity, masked,
-                                                              seen, row);
-                if (!ok) return false;
-            }
+            if (active && !softmax_step<kDtype, kHalves>(g, sh, lanes + stream * 128 + buf * 64, lanes + 256 + stream * 128, first,
+                                                         &sh->pv_done[stream][buf ^ 1], (count - 1) >> 1 & 1, masked, seen, row))
+                return false;
             first = false;
             tc_fence_before();
-            mbar_arrive(&sh->p_full[stream]);
-            ++steps_done;
+            mbar_arrive(&sh->p_full[stream][buf]);
+            ++count;
         }
-        if (!first && !warp_wait(&sh->pv_done[stream], (steps_done - 1) & 1, sh, a.err_word)) return false;
+        // (A buffer's products are done when its next scores are there, so that this phase is the current one or the last.)
+        if (!warp_wait(&sh->pv_done[stream][(count - 1) & 1], (count - 1) >> 1 & 1, sh, a.err_word)) return false;
         // the two streams of one query tile are joined: each warp group takes every other 32 columns
         float w[2] = {1.f, 0.f};
         if (!two) {
@@ -859,7 +859,7 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             row.sum = sh->stat[0][lane_row][1] * w[0] + sh->stat[1][lane_row][1] * w[1];
         }
         tc_fence_after();
-        const bool join = !two && u.t1 - u.t0 > 1, bad = sh->not_finite[u.index % kUnitFlags] != 0;
+        const bool bad = sh->not_finite[u.index % kUnitFlags] != 0;
         if (active) {
             const float inv = row.sum == 0.f ? 0.f : 1.f / row.sum;
             const float lse = row.sum == 0.f ? -INFINITY : row.top * kLn2 + logf(row.sum);
@@ -880,7 +880,7 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
                 tmem_ld32_async(lanes + 384 + c + 32, o, 96);
                 tmem_ld_wait(o);
 #pragma unroll
-                for (int i = 0; i < 64; ++i) o[i] = join ? fmaf(o[64 + i], w[1], o[i] * w[0]) : o[i] * w[0];
+                for (int i = 0; i < 64; ++i) o[i] = !two ? fmaf(o[64 + i], w[1], o[i] * w[0]) : o[i] * w[0];
                 if (r < u.rows) {
 #pragma unroll
                     for (int i = 0; i < 64; i += 8) {
@@ -932,9 +932,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh->q_full[i], kLoadThreads);
             mbar_init(&sh->q_empty[i], 1);
-            mbar_init(&sh->s_full[i], 1);
-            mbar_init(&sh->p_full[i], kTileRows);
-            mbar_init(&sh->pv_done[i], 1);
+            for (int j = 0; j < 2; ++j) {
+                mbar_init(&sh->s_full[i][j], 1);
+                mbar_init(&sh->p_full[i][j], kTileRows);
+                mbar_init(&sh->pv_done[i][j], 1);
+            }
         }
         for (int i = 0; i < R::kK; ++i) {
             mbar_init(&sh->k_full[i], kTileArrivals);
@@ -1152,7 +1154,7 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     const bool bf16 = a->dtype == SPEC_BF16;
     const uint32_t type = bf16 ? 1u << 7 | 1u << 10 : 0u;              // A and B: bf16 or fp16
     const uint32_t common = 1u << 4 | type | (uint32_t)(kTileRows >> 4) << 24;
-    g.desc_qk = common | (uint32_t)(kTileKeys >> 3) << 17 | (a->scale < 0.f ? 1u << 13 : 0u);       // a negative scale negates Q
+    g.desc_qk = common | (uint32_t)(kStepKeys >> 3) << 17 | (a->scale < 0.f ? 1u << 13 : 0u);       // a negative scale negates Q
     g.desc_pv = common | (uint32_t)((a->D + 15) / 16 * 2) << 17 | 1u << 16;                         // V is MN-major
     g.part_rows = part_rows(a->T, a->Hq, a->Hkv);
     g.joins = (Join *)workspace;
