@@ -74,7 +74,7 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
     const PlanSmem lay = plan_smem(K, n, T);
     unsigned long long *keys = (unsigned long long *)(smem + lay.keys);
     int *low = (int *)(smem + lay.low), *first = (int *)(smem + lay.first), *number = (int *)(smem + lay.number);
-    int *up = (int *)(smem + lay.parent);
+    int *up = (int *)(smem + lay.parent);                // (number: the tokens first, then the entries of the table)
     const int b = blockIdx.x, t = threadIdx.x, threads = blockDim.x;
     cand += (size_t)b * K * n;
     tok += (size_t)b * T;
@@ -82,6 +82,8 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
     parent += (size_t)b * T;
     node_of += (size_t)b * K * (n + 1);
 
+    const int length = seq_len[b], root = last_tok[b];
+    for (int i = t; i < K * n; i += threads) number[i] = cand[i];        // one latency of HBM, not one per level
     for (int j = 0; j < n; ++j) {
         for (int i = t; i < lay.slots; i += threads) {
             keys[i] = 0;
@@ -89,7 +91,7 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
         }
         __syncthreads();
         for (int k = t; k < K; k += threads) {
-            const int with = j == 0 ? 0 : first[k * n + j - 1], c = cand[k * n + j];
+            const int with = j == 0 ? 0 : first[k * n + j - 1], c = number[k * n + j];
             int at = -1;
             if (with >= 0 && c >= 0) {
                 const unsigned long long key = ((unsigned long long)(with + 1) << 32) | (uint32_t)c;
@@ -118,7 +120,6 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
     for (int i = begin; i < end; ++i)
         if (first[i] == i / n) number[i] = next++;
     const int nodes = min(1 + total, T);
-    const int length = seq_len[b];
     __syncthreads();
     for (int i = t; i < K * n; i += threads) {
         const int k = i / n, j = i - k * n;
@@ -135,7 +136,7 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
     }
     for (int i = t; i < T; i += threads) {
         if (i != 0 && i < nodes) continue;
-        tok[i] = i == 0 ? last_tok[b] : 0;
+        tok[i] = i == 0 ? root : 0;
         parent[i] = -1;
         pos[i] = length;
         up[i] = -1;
