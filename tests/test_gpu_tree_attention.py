@@ -76,7 +76,8 @@ def test_single_tokens(spec, D, lens, dtype):
     Case(len(lens), 1, 4, 2, D, lens, 16, dtype, levels=0).run_and_check(spec)
 
 
-@pytest.mark.parametrize("page,layout", [(1, "nhd"), (7, "hnd"), (8, "nhd"), (16, "hnd"), (24, "nhd"), (64, "hnd"), (200, "nhd")])
+@pytest.mark.parametrize("page,layout", [(1, "nhd"), (7, "hnd"), (8, "nhd"), (16, "hnd"), (24, "nhd"), (64, "hnd"), (200, "nhd"),
+                                         (32, "nhd"), (128, "hnd"), (256, "nhd"), (384, "hnd")])
 @pytest.mark.parametrize("T,lens,nodes", [(5, [250, 3], None), (33, [0, 100], [33, 20]), (61, [511, 90], [1, 61])])
 def test_pages_that_end_inside_a_tile(spec, page, layout, T, lens, nodes):
     Case(2, T, 4, 4, 64, lens, page, layout=layout, nodes=nodes).run_and_check(spec)
@@ -181,6 +182,39 @@ def test_strides(spec):
     out = torch.full((6, 3, 7, 72), 7.0, dtype=torch.bfloat16, device="cuda")
     c.run_and_check(spec, out=out[..., 8:].permute(1, 2, 0, 3))
     assert (out[..., :8] == 7).all()
+
+
+@pytest.mark.parametrize("page", [16, 24, 256])
+def test_keys_and_values_interleaved_in_one_pool(spec, page):
+    c = Case(2, 11, 4, 2, 128, [700, 390], page)
+    pool = torch.full((c.k_cache.shape[0], 2, page, 2, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    pool[:, 0], pool[:, 1] = c.k_cache, c.v_cache
+    c.k_cache, c.v_cache = pool[:, 0], pool[:, 1]
+    c.run_and_check(spec)
+
+
+@pytest.mark.parametrize("T", [7, 130])
+def test_one_head_of_keys_seen_as_several(spec, T):
+    """Expanded inputs: what TMA does not take as a tensor comes row by row."""
+    c = Case(2, T, 4, 1, 64, [300, 129], 16)
+    c.k, c.v = c.k.expand(-1, -1, 4, -1), c.v.expand(-1, -1, 4, -1)
+    c.k_cache, c.v_cache = c.k_cache.expand(-1, -1, 4, -1), c.v_cache.expand(-1, -1, 4, -1)
+    c.shape = (2, T, 4, 4, 64)
+    c.run_and_check(spec)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(spec, seed):
+    """Lengths, trees, heads and pages at random: units of every kind side by side, in one CTA and across several."""
+    rng = np.random.default_rng(100 + seed)
+    Hkv = int(rng.choice([1, 2, 3, 5]))
+    T = int(rng.choice([1, 2, 17, 40, 90, 200]))
+    B = int(rng.integers(1, 9))
+    G = int(rng.choice([1, 2, 4, 9] if T < 90 else [1, 2]))
+    lens = np.where(rng.random(B) < 0.3, rng.integers(0, 130, B), rng.integers(0, int(rng.choice([300, 3000, 9000])), B))
+    Case(B, T, G * Hkv, Hkv, int(rng.choice([64, 88, 128])), lens, int(rng.choice([5, 8, 16, 64, 128])),
+         torch.bfloat16 if seed % 2 else torch.float16, layout=["nhd", "hnd"][seed // 2 % 2], levels=int(rng.choice([0, 1, 4])),
+         nodes=rng.integers(0, T + 1, B), empty_rows=0.1 * (seed % 3 == 0), seed=seed).run_and_check(spec)
 
 
 def test_defaults(spec):
