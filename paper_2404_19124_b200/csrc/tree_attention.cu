@@ -3,22 +3,30 @@
 //
 // Work.  A unit is a sequence, a key head and up to 256 of the query rows that share it (row = node * group + head within the
 // group); its keys, the cache's and then the tree's, are cut into tiles of 128.  All tiles of all units in a row are dealt to
-// the CTAs, one per SM, in runs of equal cost (a tile costs 2 for units of more than 128 rows, else 1; see Deal), so that ragged batches and
-// few long sequences fill the GPU alike.  A unit that a CTA has to itself is written straight to `out`; of the others every CTA
-// leaves its rows, normalised, with their log-sum-exp in the workspace, and tree_combine_kernel joins them.  (Lengths are read on the device: a captured launch serves any.)
+// the CTAs, one per SM, in runs of equal cost (see Deal), so that ragged batches and few long sequences fill the GPU alike.  A unit
+// that a CTA has to itself is written straight to `out`; of the others every CTA leaves its rows, normalised, with their
+// log-sum-exp in the workspace, and tree_combine_kernel joins them.  Lengths are read on the device: a captured launch
+// serves any.
 //
 // Roles of a CTA (16 warps):
 //   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
 //                   TMEM in place of the scores, results
-//   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 128], O += P V, P read from TMEM
+//   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 64], O += P V, P read from TMEM
 //   warps 9-11      bring the tiles of K and V that lie in the cache, as TMA boxes: a page (or 128 tokens of one) by 64 columns
 //   warps 12-15     bring the others row by row with 16-byte asynchronous copies (rows that do not exist read as zeros): Q, the tile
 //                   in which the cache ends and the tree begins, the tree, and caches whose pages do not tile 128 keys
 // Tiles are 128-byte-swizzled either way.
+//
 // Two streams of softmax, 64 keys at a step, each with two score buffers, so that the scores of the next step are there when one
 // is done and the products of the last step run meanwhile.  (With one buffer of 128 keys per stream neither the tensor cores, 43 %
 // busy, nor the exponentials, 39 %, were the limit, but the way round.)  Units of more than 128 rows have a stream per 128
 // rows, which take both halves of every tile of keys; in smaller ones each stream takes a half, and the two results are joined.
+//
+// What bounds it.  Up to 128 rows per key head, the keys' way from HBM: 131072 tokens of one sequence 113 us, 4.75 TB/s of
+// 6.5; 16 sequences with 40 key heads and trees of 31 to 61 nodes 117 us, 3.5 TB/s (units of 10 tiles, whose ends nothing hides).
+// With more rows the chain scores - softmax - products of a step and the power cap: 64 sequences, trees of 65 to 129 nodes,
+// four query heads per key head 368 us from a cool start, 400 to 420 on and on (1.6 GHz), 0.55 of 1.63 PFLOP/s.  Few tiles:
+// latency, 22 us for single tokens of 4 sequences, of which the second kernel is 4.
 #include <limits.h>
 #include <math.h>
 
@@ -37,7 +45,6 @@ using tc::mbar_init;
 using tc::smem_u32;
 using tc::tc_fence_after;
 using tc::tc_fence_before;
-using tc::tmem_ld32;
 using tc::umma_commit;
 
 constexpr int kTileKeys = 128;
@@ -51,10 +58,10 @@ constexpr int kFirstLoader = kSoftmaxThreads + 32 * (1 + kBoxWarps);
 constexpr int kThreads = kFirstLoader + kLoadThreads;
 // A tile of K or V is complete after kBoxWarps arrivals of kLoadThreads each (TMA) or kLoadThreads of kBoxWarps each (copies).
 constexpr int kTileArrivals = kBoxWarps * kLoadThreads;
-// Registers of a thread after the roles have parted; 2 * 128 * (184 + 72) is what the launch has (512 threads of 128).  (All that the
+// Registers of a thread after the roles have parted; 2 * 128 * (192 + 64) is what the launch has (512 threads of 128).  (All that the
 // roles call is inlined: around a call the compiler does not go beyond the launch's 128.)
 constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
-constexpr int kTmemCols = 512;                  // S0, S1, O0, O1: 128 columns each
+constexpr int kTmemCols = 512;                  // 128 columns each: the two buffers of S0, of S1, then O0, O1
 constexpr int kUnitFlags = 8;
 constexpr uint64_t kWaitMaxNs = 1000000000;     // after which a wait gives up
 constexpr uint32_t kWaitHintNs = 20000;
@@ -93,7 +100,7 @@ struct Shared {
     uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], meet, drained, boxes_asked, rows_asked;
     uint32_t tmem_base;
     volatile int abort_flag;
-    volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see load_v)
+    volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see finite_values)
     int start_b;
     long long start_off, left;
     Deal deal;
