@@ -8,12 +8,14 @@
 // log-sum-exp in the workspace, and tree_combine_kernel joins them.  Lengths are read on the device: a captured launch
 // serves any.
 //
-// Roles of a CTA (16 warps):
+// Roles of a CTA (20 warps):
 //   warps 0-3, 4-7  softmax of stream 0 and 1, a thread per row: scores from TMEM, running maximum and sum, probabilities back to
 //                   TMEM in place of the scores, results
-//   warp 8          TMEM allocation; one lane issues the MMAs:  S = Q K^T [128 x 64], O += P V, P read from TMEM
-//   warps 9-11      bring the tiles of K and V that lie in the cache, as TMA boxes: a page (or 128 tokens of one) by 64 columns
-//   warps 12-15     bring the others row by row with 16-byte asynchronous copies (rows that do not exist read as zeros): Q, the tile
+//   warps 8, 9      one lane issues the MMAs of stream 0 and of stream 1:  S = Q K^T [128 x 64], O += P V, P read from TMEM; a
+//                   lane for both spent as long on waits and commits as the tensor cores on the products.  Warp 8 allocates TMEM
+//   warps 10, 11    nothing (registers are given away by groups of four warps)
+//   warps 12-15     bring the tiles of K and V that lie in the cache, as TMA boxes: a page (or 128 tokens of one) by 64 columns
+//   warps 16-19     bring the others row by row with 16-byte asynchronous copies (rows that do not exist read as zeros): Q, the tile
 //                   in which the cache ends and the tree begins, the tree, and caches whose pages do not tile 128 keys
 // Tiles are 128-byte-swizzled either way.
 //
@@ -52,15 +54,18 @@ constexpr int kTileRows = 128;
 constexpr int kStepKeys = 64;
 constexpr int kHalfBytes = kTileKeys * 128;     // 64 columns of a tile of 128 rows
 constexpr int kSoftmaxThreads = 256;
-constexpr int kBoxWarps = 3;
+constexpr int kMmaWarp = kSoftmaxThreads / 32, kBoxWarp = kMmaWarp + 4;        // the first of each
+constexpr int kBoxWarps = 4;
 constexpr int kLoadThreads = 128;
-constexpr int kFirstLoader = kSoftmaxThreads + 32 * (1 + kBoxWarps);
+constexpr int kFirstLoader = 32 * (kBoxWarp + kBoxWarps);
 constexpr int kThreads = kFirstLoader + kLoadThreads;
 // A tile of K or V is complete after kBoxWarps arrivals of kLoadThreads each (TMA) or kLoadThreads of kBoxWarps each (copies).
 constexpr int kTileArrivals = kBoxWarps * kLoadThreads;
-// Registers of a thread after the roles have parted; 2 * 128 * (192 + 64) is what the launch has (512 threads of 128).  (All that the
-// roles call is inlined: around a call the compiler does not go beyond the launch's 128.)
-constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
+// Registers of a thread after the roles have parted; 128 * (2 * 160 + 48 + 48 + 64) is what the launch has (640 threads of 96).  (All
+// that the roles call is inlined: around a call the compiler does not go beyond the launch's 96.)  Spills cost more than warps
+// bring: with 168 for the softmax and 48 for the rest the 13B trees took 132 us instead of 113.
+constexpr int kSoftmaxRegs = 160, kMmaRegs = 48, kBoxRegs = 48, kRowRegs = 64;
+static_assert(2 * kSoftmaxRegs + kMmaRegs + kBoxRegs + kRowRegs <= 5 * 96, "registers of the launch");
 constexpr int kTmemCols = 512;                  // 128 columns each: the two buffers of S0, of S1, then O0, O1
 constexpr int kUnitFlags = 8;
 constexpr uint64_t kWaitMaxNs = 1000000000;     // after which a wait gives up
@@ -435,7 +440,7 @@ __device__ __forceinline__ void pass_over(int n, int &slot, uint32_t &parity) {
 template <int kHalves>
 __device__ void box_role(const AttnArgs &g, Shared *sh, uint32_t k_tiles, uint32_t v_tiles) {
     using R = Ring<kHalves>;
-    const int warp = (threadIdx.x >> 5) - (kSoftmaxThreads / 32 + 1), lane = threadIdx.x & 31;
+    const int warp = (threadIdx.x >> 5) - kBoxWarp, lane = threadIdx.x & 31;
     int ks = 0, vs = 0;                                  // slots, and the parity of their `empty` that means free
     uint32_t kp = 1, vp = 1, rows_parity = 0;
     uint64_t once = tc::evict_first_policy(), normal;
@@ -587,72 +592,75 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 }
 
 template <int kHalves>
-__device__ bool mma_role(const AttnArgs &g, Shared *sh, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
+__device__ bool mma_role(const AttnArgs &g, Shared *sh, int stream, uint32_t q_tiles, uint32_t k_tiles, uint32_t v_tiles) {
     using R = Ring<kHalves>;
     int32_t *err = g.a.err_word;
-    const uint32_t tmem = sh->tmem_base;
+    const uint32_t s_cols = sh->tmem_base + stream * 128, o_cols = sh->tmem_base + 256 + stream * 128;
+    const uint32_t desc_qk = g.desc_qk, desc_pv = g.desc_pv;
     const int k_steps = (g.a.D + 15) / 16;
     int qs = 0, ks = 0, vs = 0;
     uint32_t qp = 0, kp = 0, vp = 0;
-    uint32_t count = 0;                                  // steps of either stream in the units before
+    uint32_t count = 0;                                  // steps of the stream in the units before; buffers go by it
     Walk walk(g, sh);
     Unit u;
     while (walk.next(g, u)) {
-        // step j: stream j & 1, its buffer by its own count.  two: tile j / 4, half (j / 2) & 1; else tile j / 2, half j & 1
+        // two: step i is half i & 1 of tile i / 2; else half `stream` of tile i
         const bool two = u.two_tiles();
-        const int steps = (u.t1 - u.t0) * (two ? 4 : 2);
-        const int q0 = qs, q1 = two ? qs ^ 1 : qs;       // slots of the unit's query tiles
-        const uint32_t qp0 = qp, qp1 = two && qs == 1 ? qp ^ 1 : qp;
+        const int steps = (u.t1 - u.t0) * (two ? 2 : 1), boxed = boxed_tiles(g, u) - u.t0;
+        const int q = two && stream ? qs ^ 1 : qs;       // the stream's query tile
+        const uint32_t q_parity = two && stream && qs == 1 ? qp ^ 1 : qp;
         if (!two) {
             if (++qs == R::kQ) qs = 0, qp ^= 1;
         } else {
             qp ^= 1;
         }
-        auto scores = [&](int j) -> bool {
-            const int s = j & 1, half = two ? j >> 1 & 1 : s, q = s ? q1 : q0;
-            const uint32_t buf = (count + (j >> 1)) & 1;
-            if (j < 2 && !wait(&sh->q_full[q], s ? qp1 : qp0, sh, err)) return false;
+        const uint64_t qd = tc::make_smem_desc(q_tiles + q * R::kBytes);
+        auto scores = [&](int i) -> bool {
+            const int half = two ? i & 1 : stream;
+            const uint32_t buf = (count + i) & 1;
+            if (i == 0 && !wait(&sh->q_full[q], q_parity, sh, err)) return false;
             if (!wait(&sh->k_full[ks], kp, sh, err)) return false;
-            fence_async_proxy();
+            if (i == 0 || (two ? i >> 1 : i) >= boxed) fence_async_proxy();      // Q and such tiles are written by ordinary copies
             // (Unrolled, with descriptors that differ by constants: a loop that builds them took 140 cycles an MMA, twice its time.)
-            const uint64_t qd = tc::make_smem_desc(q_tiles + q * R::kBytes);
             const uint64_t kd = tc::make_smem_desc(k_tiles + ks * R::kBytes + half * kStepKeys * 128);
-            const uint32_t d = tmem + s * 128 + buf * 64, desc = g.desc_qk;
+            const uint32_t d = s_cols + buf * 64;
 #pragma unroll
-            for (int i = 0; i < 4 * kHalves; ++i) {
+            for (int n = 0; n < 4 * kHalves; ++n) {
                 constexpr int kHalf = kHalfBytes >> 4;
-                const int off = (i >> 2) * kHalf + (i & 3) * 2;
-                if (i < k_steps) mma_ss(d, qd + off, kd + off, desc, i > 0);
+                const int off = (n >> 2) * kHalf + (n & 3) * 2;
+                if (n < k_steps) mma_ss(d, qd + off, kd + off, desc_qk, n > 0);
             }
-            umma_commit(&sh->s_full[s][buf]);
-            if (s && (!two || half)) {
+            umma_commit(&sh->s_full[stream][buf]);
+            if (!two || half) {
                 umma_commit(&sh->k_empty[ks]);
                 if (++ks == R::kK) ks = 0, kp ^= 1;
             }
-            if (j == steps - 1 || (two && j == steps - 2)) umma_commit(&sh->q_empty[q]);
+            if (i == steps - 1) {                        // a slot of Q is free when both streams say so
+                umma_commit(&sh->q_empty[q]);
+                if (two) umma_commit(&sh->q_empty[q ^ 1]);
+            }
             return true;
         };
-        for (int j = 0; j < 4 && j < steps; ++j)
-            if (!scores(j)) return false;
-        for (int j = 0; j < steps; ++j) {
-            const int s = j & 1, half = two ? j >> 1 & 1 : s;
-            const uint32_t at = count + (j >> 1), buf = at & 1;
-            if (!wait(&sh->p_full[s][buf], at >> 1 & 1, sh, err)) return false;
+        if (!scores(0) || (steps > 1 && !scores(1))) return false;
+        for (int i = 0; i < steps; ++i) {
+            const int half = two ? i & 1 : stream;
+            const uint32_t at = count + i, buf = at & 1;
             if (!wait(&sh->v_full[vs], vp, sh, err)) return false;
-            fence_async_proxy();
+            if ((two ? i >> 1 : i) >= boxed) fence_async_proxy();
+            if (!wait(&sh->p_full[stream][buf], at >> 1 & 1, sh, err)) return false;
             tc_fence_after();
             const uint64_t vd = v_desc(v_tiles + vs * R::kBytes + half * kStepKeys * 128);
-            const uint32_t d = tmem + 256 + s * 128, pa = tmem + s * 128 + buf * 64, desc = g.desc_pv;
+            const uint32_t pa = s_cols + buf * 64;
 #pragma unroll
-            for (int i = 0; i < kStepKeys / 16; ++i) mma_ts(d, pa + i * 8, vd + i * (2048 >> 4), desc, j >= 2 || i > 0);
-            umma_commit(&sh->pv_done[s][buf]);
-            if (s && (!two || half)) {
+            for (int n = 0; n < kStepKeys / 16; ++n) mma_ts(o_cols, pa + n * 8, vd + n * (2048 >> 4), desc_pv, i > 0 || n > 0);
+            umma_commit(&sh->pv_done[stream][buf]);
+            if (!two || half) {
                 umma_commit(&sh->v_empty[vs]);
                 if (++vs == R::kV) vs = 0, vp ^= 1;
             }
-            if (j + 4 < steps && !scores(j + 4)) return false;
+            if (i + 2 < steps && !scores(i + 2)) return false;
         }
-        count += steps / 2;
+        count += steps;
     }
     return true;
 }
@@ -798,7 +806,7 @@ __device__ __forceinline__ bool softmax_step(const AttnArgs &g, Shared *sh, uint
 }
 
 // What finite_values kept out of the products: values that are not finite, of the nodes that the row sees, are added to the row's
-// result in memory, which its own thread has just written (columns col0 .. col0 + 63).
+// result in memory, which its own thread has just written (columns col0 .. col0 + 31).
 template <int kDtype>
 __device__ __forceinline__ void add_not_finite(const spec_tree_attention_t &a, const Unit &u, const RowMask &mask, int col0,
                                             uint16_t *out, float *part) {
@@ -806,7 +814,7 @@ __device__ __forceinline__ void add_not_finite(const spec_tree_attention_t &a, c
     for (int n = first; n < end; ++n) {
         if (!(mask.bits(n) & 1)) continue;
         const uint16_t *v = (const uint16_t *)a.v + u.b * a.v_stride[0] + n * a.v_stride[1] + u.head * a.v_stride[2];
-        for (int i = col0; i < min(col0 + 64, a.D); ++i) {
+        for (int i = col0; i < min(col0 + 32, a.D); ++i) {
             const float x = number<kDtype>(v[i], 0);
             if (fabsf(x) < INFINITY) continue;
             if (part != nullptr) part[i] += x;
@@ -885,20 +893,18 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
             const bool whole = u.whole();
             w[0] *= inv;
             w[1] *= inv;
-            // 64 columns at a time, of both streams, behind one wait: a load of TMEM takes several hundred cycles while MMAs run
+            // 32 columns at a time, of both streams, behind one wait: a load of TMEM takes several hundred cycles while MMAs run
 #pragma unroll 1
-            for (int c = two ? 0 : stream * 64; c < (two ? a.D : min(a.D, stream * 64 + 64)); c += 64) {
-                float o[128];
+            for (int c = two ? 0 : stream * 32; c < a.D; c += two ? 32 : 64) {
+                float o[64];
                 tmem_ld32_async(lanes + 256 + (two ? stream * 128 : 0) + c, o, 0);
-                tmem_ld32_async(lanes + 256 + (two ? stream * 128 : 0) + c + 32, o, 32);
-                tmem_ld32_async(lanes + 384 + c, o, 64);
-                tmem_ld32_async(lanes + 384 + c + 32, o, 96);
+                tmem_ld32_async(lanes + 384 + c, o, 32);
                 tmem_ld_wait(o);
 #pragma unroll
-                for (int i = 0; i < 64; ++i) o[i] = !two ? fmaf(o[64 + i], w[1], o[i] * w[0]) : o[i] * w[0];
+                for (int i = 0; i < 32; ++i) o[i] = !two ? fmaf(o[32 + i], w[1], o[i] * w[0]) : o[i] * w[0];
                 if (r < u.rows) {
 #pragma unroll
-                    for (int i = 0; i < 64; i += 8) {
+                    for (int i = 0; i < 32; i += 8) {
                         if (c + i >= a.D) continue;
                         if (whole) {
                             uint4 y;
@@ -946,7 +952,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh->q_full[i], kLoadThreads);
-            mbar_init(&sh->q_empty[i], 1);
+            mbar_init(&sh->q_empty[i], 2);
             for (int j = 0; j < 2; ++j) {
                 mbar_init(&sh->s_full[i][j], 1);
                 mbar_init(&sh->p_full[i][j], kTileRows);
@@ -955,14 +961,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         for (int i = 0; i < R::kK; ++i) {
             mbar_init(&sh->k_full[i], kTileArrivals);
-            mbar_init(&sh->k_empty[i], 1);
+            mbar_init(&sh->k_empty[i], 2);
         }
         for (int i = 0; i < R::kV; ++i) {
             mbar_init(&sh->v_full[i], kTileArrivals);
-            mbar_init(&sh->v_empty[i], 1);
+            mbar_init(&sh->v_empty[i], 2);
         }
         mbar_init(&sh->meet, kSoftmaxThreads);
-        mbar_init(&sh->drained, 1);
+        mbar_init(&sh->drained, 2);
         mbar_init(&sh->boxes_asked, kBoxWarps);
         mbar_init(&sh->rows_asked, kLoadThreads / 32);
         sh->abort_flag = 0;
@@ -994,17 +1000,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         softmax_role<kDtype, kHalves>(g, sh);
-    } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == 8 && tc::elect_one()) {
-            mma_role<kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
+    } else if (warp < kBoxWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+        if (warp < kMmaWarp + 2 && tc::elect_one()) {
+            mma_role<kHalves>(g, sh, warp - kMmaWarp, q_tiles, k_tiles, v_tiles);
             umma_commit(&sh->drained);                   // what was issued ends before TMEM and shared memory go
             for (const uint64_t start = now_ns(); !try_wait(&sh->drained, 0) && now_ns() - start < kWaitMaxNs;) {}
         }
-        if (warp > 8) box_role<kHalves>(g, sh, k_tiles, v_tiles);
         __syncwarp();
+    } else if (warp < kBoxWarp + kBoxWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBoxRegs));
+        box_role<kHalves>(g, sh, k_tiles, v_tiles);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRowRegs));
         row_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
         asm volatile("cp.async.wait_all;" ::: "memory");
     }
