@@ -744,7 +744,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 
 // One step of a row: probabilities in place of the scores.  The maximum follows the steps lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
-// saves nearly every pass over the accumulated output (a pass waits for the products of the step before).
+// saves nearly every pass over the accumulated output (a pass waits for the products of the step before).  The probabilities are
+// rounded to the 16 bits that the tensor cores take beside the values, each by half a step at most; their sum is not.
 template <int kDtype, int kHalves>
 __device__ __forceinline__ bool softmax_step(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
                                              uint64_t *pv_done, uint32_t pv_parity, bool masked, uint64_t seen, Row &row) {
