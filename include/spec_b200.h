@@ -382,7 +382,7 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
  *   mask         dev uint32 [B, T, ceil(T / 32)] as spec_tree_plan writes it, or NULL: node i sees nodes 0 .. i (a chain)
  *   lse          dev fp32 [B, T, Hq], or NULL
  *   workspace    dev, 256-byte aligned, >= spec_tree_attention_workspace_bytes(...); need not be zeroed.  Calls that may
- *                overlap on the GPU need workspaces of their own.
+ *                overlap on the GPU need workspaces of their own.  `out` and `lse` must not overlap the inputs.
  * Limits: D a multiple of 8, at most 128; Hq a multiple of Hkv; T <= SPEC_MAX_TREE_NODES; else SPEC_ERR_SHAPE.
  * Lengths out of [0, max_pages * page_size] and node counts out of [0, T] are clamped, a page id outside [0, n_pages) reads as
  * zeros, and err_word receives SPEC_ERR_INDEX_RANGE. */
@@ -441,7 +441,7 @@ int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
 /* ---- spec_kv_commit: the accepted path's keys and values
  *     k_cache[l, page, offset] = k[l, b, path[b, j]],  v likewise,  for j = 0 .. accept_len[b], slots[b, j] = (page, offset)
  *     new_len[b] = seq_len[b] + accept_len[b] + 1
- * for all L layers in one launch.  16-bit elements of any type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
+ * for all L layers in one launch (k, v must not overlap the caches; of equal slots any row may stay).  16-bit elements of any type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
  *   k, v         dev [L, B, T, H, D], strides (layer, sequence, node, head)
  *   k_cache, v_cache  dev [L, n_pages, page_size, H, D], strides (layer, page, token, head)
  *   path         dev int32 [B, n + 1], accept_len dev int32 [B]   as spec_verify_tree writes them
