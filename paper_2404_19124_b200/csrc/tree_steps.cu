@@ -402,10 +402,12 @@ __device__ __forceinline__ float walk_adjust(const WalkArgs &a, const WalkTable 
     return x;
 }
 
-// Eight consecutive bits of a bit field of `bytes` bytes, from `first` on.
+// Eight consecutive bits of a bit field of `bytes` bytes, from `first` on, which is a multiple of 4 or, unless kAligned, anything.
+template <bool kAligned>
 __device__ __forceinline__ uint32_t bits_from(const uint32_t *field, int first, int bytes) {
     const uint8_t *p = (const uint8_t *)field;
     uint32_t x = p[first >> 3];
+    if (kAligned) return x >> (first & 4);
     if (first & 7) {
         if ((first >> 3) + 1 < bytes) x |= (uint32_t)p[(first >> 3) + 1] << 8;
         x >>= first & 7;
@@ -413,32 +415,34 @@ __device__ __forceinline__ uint32_t bits_from(const uint32_t *field, int first, 
     return x & 0xffu;
 }
 
-// A vector with what `use` does not keep at minus infinity.
+// A vector with what `use` does not keep at minus infinity.  keep: for each of 256 values of `use` the 16-bit elements that stay.
 template <int kDtype>
-__device__ __forceinline__ void blank(uint4 &x, uint32_t use) {
-    constexpr uint32_t kNone = kDtype == SPEC_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+__device__ __forceinline__ void blank(uint4 &x, uint32_t use, const uint4 *keep) {
+    if (kDtype == SPEC_F32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t &w = (&x.x)[i];
-        if (kDtype == SPEC_F32) {
-            if (!(use >> i & 1)) w = 0xff800000u;
-        } else {
-            const uint32_t keep = (use >> 2 * i & 1) * 0xffffu | (use >> (2 * i + 1) & 1) * 0xffff0000u;
-            w = (w & keep) | (kNone & ~keep);
-        }
+        for (int i = 0; i < 4; ++i)
+            if (!(use >> i & 1)) (&x.x)[i] = 0xff800000u;
+    } else {
+        constexpr uint32_t kNone = kDtype == SPEC_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+        const uint4 k = keep[use];
+        x.x = (x.x & k.x) | (kNone & ~k.x);
+        x.y = (x.y & k.y) | (kNone & ~k.y);
+        x.z = (x.z & k.z) | (kNone & ~k.z);
+        x.w = (x.w & k.w) | (kNone & ~k.w);
     }
 }
 
 // The maximum over this CTA's blocks of a row, of the tokens that `allow` (null: all) and `marked` (null: none) leave.  A thread's
 // vectors rise and four of them (and the grammar's bits) are in flight.  It keeps the vector with the greatest maximum, without a
 // branch, and looks for the element at the end: a branch for every new maximum is taken by some lane nearly always.
-template <int kDtype>
+// kAligned: the row begins at a vector, so that no vector holds elements of two blocks or two bytes of bits.
+template <int kDtype, bool kAligned>
 __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uint32_t rank, const uint32_t *allow, int words,
-                                         const uint32_t *marked, Best &best) {
+                                         const uint32_t *marked, const uint4 *keep, Best &best) {
     constexpr int kPer = 16 / Logit<kDtype>::kBytes, kPerThread = kBlockTokens / kPer / kWalkThreads, kAhead = 4;
     constexpr uint32_t kAll = (1u << kPer) - 1;
     const int V = a.v.V;
-    const int skew = (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);       // elements behind a vector's start
+    const int skew = kAligned ? 0 : (int)(((uintptr_t)row & 15) / Logit<kDtype>::kBytes);        // elements behind a vector's start
     const uint4 *vec = (const uint4 *)(row - skew * Logit<kDtype>::kBytes);
     const int blocks = (V + kBlockTokens - 1) / kBlockTokens;
     const int turns = (blocks - (int)rank + (1 << a.log_ctas) - 1) >> a.log_ctas;
@@ -448,11 +452,11 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
     int best_e0 = 0;
     auto first_of = [&](int turn) { return ((turn << a.log_ctas) + (int)rank) * kBlockTokens; };
     auto look = [&](uint4 x, int e0, int begin, int turn, uint32_t use) {        // use: the grammar's bits from max(e0, begin) on
-        const int from = max(e0, begin);
+        const int from = kAligned ? e0 : max(e0, begin);
+        if (marked != nullptr) use &= ~bits_from<kAligned>(marked, turn * kBlockTokens + from - begin, a.part / 8);
         use = use << (from - e0) & kAll;
-        if (e0 + kPer > begin + kBlockTokens) use &= kAll >> (e0 + kPer - begin - kBlockTokens);
+        if (!kAligned && e0 + kPer > begin + kBlockTokens) use &= kAll >> (e0 + kPer - begin - kBlockTokens);
         if (e0 + kPer > V) use &= kAll >> (e0 + kPer - V);
-        if (marked != nullptr) use &= ~(bits_from(marked, turn * kBlockTokens + from - begin, a.part / 8) << (from - e0));
         if (e0 < 0 || e0 + kPer > V) {                   // a vector that reaches beyond the row: the memory there may be nobody's
             uint32_t y[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -463,7 +467,7 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
             }
             x = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        if (use != kAll) blank<kDtype>(x, use);
+        if (use != kAll) blank<kDtype>(x, use, keep);
         const float top = fmaxf(Logit<kDtype>::most(x), -INFINITY);
         const bool take = use != 0 && (best_use == 0 || top > best_top);
         best_top = take ? top : best_top;
@@ -485,7 +489,7 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
             x[k] = make_uint4(0, 0, 0, 0);
             if (turn >= turns || e0 >= V) continue;
             if (e0 >= 0 && e0 + kPer <= V) x[k] = __ldg((const uint4 *)((const char *)vec + (long long)(e0 + skew) * Logit<kDtype>::kBytes));
-            if (allow != nullptr) use[k] = bits_from(allow, max(e0, begin), words * 4);
+            if (allow != nullptr) use[k] = bits_from<kAligned>(allow, kAligned ? e0 : max(e0, begin), words * 4);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -494,13 +498,13 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
             if (turn < turns && e0 < V) look(x[k], e0, begin, turn, use[k]);
         }
     }
-    if (skew)                                            // the vectors in which blocks end
+    if (!kAligned)                                       // the vectors in which blocks end
         for (int turn = threadIdx.x; turn < turns; turn += kWalkThreads) {
             const int begin = first_of(turn), e0 = begin - skew + kBlockTokens;
             if (e0 >= V) continue;
             const uint4 x = e0 + kPer <= V ? __ldg((const uint4 *)((const char *)vec + (long long)(e0 + skew) * Logit<kDtype>::kBytes))
                                            : make_uint4(0, 0, 0, 0);
-            look(x, e0, begin, turn, allow != nullptr ? bits_from(allow, e0, words * 4) : kAll);
+            look(x, e0, begin, turn, allow != nullptr ? bits_from<kAligned>(allow, e0, words * 4) : kAll);
         }
     if (best_use == 0) return;
 #pragma unroll
@@ -513,6 +517,7 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Best warp_best[kWalkWarps];
     __shared__ __align__(8) Best peer_best[2][kWalkMaxCluster];
+    __shared__ uint4 keep[kDtype == SPEC_F32 ? 1 : 256];
     __shared__ int child[3], n_list;                     // child: of three steps in turn, so that none is cleared while it is read
     griddep_launch();
     griddep_wait();
@@ -540,6 +545,10 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
     if (t == 0) {
         n_list = 0;
         child[0] = INT_MAX;
+    }
+    if (kDtype != SPEC_F32 && t < 256) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) (&keep[t].x)[i] = (t >> 2 * i & 1) * 0xffffu | (t >> (2 * i + 1) & 1) * 0xffff0000u;
     }
     if (a.cap) {
         if (a.hashed)
@@ -588,7 +597,9 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
             const char *row = (const char *)v.logits + ((long long)b * v.logits_stride[0] + (long long)cur * v.logits_stride[1]) *
                                                            Logit<kDtype>::kBytes;
             const uint32_t *allow = v.allow == nullptr ? nullptr : v.allow + ((size_t)b * v.T + cur) * words;
-            scan_row<kDtype>(a, row, rank, allow, words, a.cap ? w.marked : nullptr, best);
+            const uint32_t *marked = a.cap ? w.marked : nullptr;
+            if (((uintptr_t)row & 15) == 0) scan_row<kDtype, true>(a, row, rank, allow, words, marked, keep, best);
+            else scan_row<kDtype, false>(a, row, rank, allow, words, marked, keep, best);
             if (a.cap) {
                 const int n = n_list;
                 for (int i = t; i < n; i += kWalkThreads) {
@@ -795,7 +806,7 @@ int spec_verify_tree(const spec_tree_verify_t *v, void *cuda_stream) {
     for (int l = most; l >= 0; --l) {
         if (!plan_walk_table(a, l, smem)) continue;
         log_ctas = l;
-        const long long per_sm = 227 * 1024 / ((long long)smem + 2048);
+        const long long per_sm = 227 * 1024 / ((long long)smem + 6144);
         if (((long long)v->B << l) <= num_sms() * (per_sm < kWalkCtasPerSm ? per_sm : kWalkCtasPerSm)) break;
     }
     if (!plan_walk_table(a, log_ctas < 0 ? 4 : log_ctas, smem)) return SPEC_ERR_SHAPE;
