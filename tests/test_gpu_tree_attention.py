@@ -298,6 +298,52 @@ def test_another_stream_and_a_captured_graph(spec):
         c.check(spec, args["out"], args["lse"])
 
 
+def test_a_batch_without_a_node(spec):
+    c = Case(3, 5, 2, 1, 64, [0, 70, 300], 16, nodes=[0, 0, 0])
+    out, lse = c.run(spec)
+    assert (out == 7).all() and (lse == 7).all() and spec.spec_poll_error(c.err) == 0
+
+
+def test_calls_on_two_streams_at_once(spec):
+    cases = [Case(4, 30, 8, 4, 128, [2000, 900, 30, 4000], 16, seed=1), Case(3, 90, 8, 2, 64, [700, 3000, 1], 64, seed=2)]
+    args, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for c in cases:
+        B, T, Hq, Hkv, D = c.shape
+        args.append(dict(out=torch.full_like(c.q, 7.0), lse=torch.full((B, T, Hq), 7.0, device="cuda"),
+                         workspace=torch.empty(spec.spec_tree_attention_workspace_bytes(B, T, Hq, Hkv, D), dtype=torch.uint8,
+                                               device="cuda"), err_workspace=torch.zeros(1, dtype=torch.int32, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, a, s in zip(cases, args, streams):
+            c.run(spec, stream=s, **a)
+    torch.cuda.synchronize()
+    for c, a in zip(cases, args):
+        c.check(spec, a["out"], a["lse"])
+
+
+def test_graphs_that_share_a_workspace_one_after_the_other(spec):
+    cases = [Case(4, 30, 8, 4, 128, [2000, 900, 30, 4000], 16, seed=1), Case(2, 30, 8, 4, 128, [700, 3000], 64, seed=2)]
+    ws = torch.empty(max(spec.spec_tree_attention_workspace_bytes(*c.shape) for c in cases), dtype=torch.uint8, device="cuda")
+    graphs, args = [], []
+    for c in cases:
+        B, T, Hq, Hkv, D = c.shape
+        args.append(dict(out=torch.full_like(c.q, 7.0), lse=torch.full((B, T, Hq), 7.0, device="cuda"), workspace=ws,
+                         err_workspace=torch.zeros(1, dtype=torch.int32, device="cuda")))
+        c.run(spec, **args[-1])
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.run(spec, **args[-1])
+    for _ in range(3):
+        for c, a, graph in zip(cases, args, graphs):
+            a["out"].fill_(7.0)
+            a["lse"].fill_(7.0)
+            graph.replay()
+        for c, a in zip(cases, args):
+            c.err = a["err_workspace"]
+            c.check(spec, a["out"], a["lse"])
+
+
 def test_results_repeat_bit_for_bit(spec):
     c = Case(5, 30, 8, 2, 128, [900, 20, 3000, 0, 411], 16)
     first = c.run(spec)
