@@ -51,8 +51,8 @@ struct PlanSmem {            // offsets in bytes
     int keys, low, first, number, parent, total;
     int slots;               // of the hash table, a power of two
 };
-__host__ __device__ inline PlanSmem plan_smem(int K, int n, int T) {
-    PlanSmem s;
+__host__ __device__ constexpr PlanSmem plan_smem(int K, int n, int T) {
+    PlanSmem s{};
     s.slots = 32;
     while (s.slots < 2 * K) s.slots *= 2;
     s.keys = 0;
@@ -63,6 +63,10 @@ __host__ __device__ inline PlanSmem plan_smem(int K, int n, int T) {
     s.total = s.parent + T * 4;
     return s;
 }
+// The most that any call asks for.  A kernel's limit belongs to the process: every call sets the same one, so that calls from
+// several host threads do not lower each other's.
+constexpr int kPlanMostSmem = plan_smem(SPEC_MAX_LEAVES, SPEC_MAX_TREE_ENTRIES / SPEC_MAX_LEAVES, SPEC_MAX_TREE_NODES).total;
+static_assert(kPlanMostSmem <= 220 * 1024 && SPEC_MAX_TREE_ENTRIES % SPEC_MAX_LEAVES == 0, "shared memory of a CTA");
 
 __global__ void __launch_bounds__(kPlanMaxThreads)
 tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *seq_len, int K, int n, int T, int32_t *tok,
@@ -261,6 +265,7 @@ constexpr int kWalkThreads = 256;
 constexpr int kWalkWarps = kWalkThreads / 32;
 constexpr int kWalkCtasPerSm = 4;            // by registers
 constexpr int kWalkMaxCluster = 16;
+constexpr size_t kWalkMostSmem = 200 * 1024; // what a CTA may ask for
 constexpr int kBlockTokens = 4096;
 constexpr int kNoToken = INT_MAX;
 constexpr uint32_t kSeen = 1u << 31;         // of a token's count: it is in the history (the rest: times it was generated)
@@ -703,7 +708,8 @@ template <int kDtype>
 int launch_walk(const WalkArgs &a, size_t smem, cudaStream_t st) {
     auto kernel = tree_walk_kernel<kDtype>;
     const int ctas = 1 << a.log_ctas;
-    SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    // (the same for every call: see kPlanMostSmem)
+    SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kWalkMostSmem));
     if (ctas > 8) SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     SPEC_CUDA_TRY(launch_pdl_cluster(kernel, dim3((unsigned)ctas * a.v.B), dim3(kWalkThreads), smem, ctas, st, a));
     return SPEC_OK;
@@ -712,7 +718,6 @@ int launch_walk(const WalkArgs &a, size_t smem, cudaStream_t st) {
 // The table of a CTA (bytes per entry: key, count, bias), the bitmap and the list.
 bool plan_walk_table(WalkArgs &a, int log_ctas, size_t &smem) {
     const spec_tree_verify_t &v = a.v;
-    constexpr size_t kMost = 200 * 1024;
     const long long blocks = ((long long)v.V + kBlockTokens - 1) / kBlockTokens;
     const long long part = (blocks + (1 << log_ctas) - 1) / (1 << log_ctas) * kBlockTokens;
     const size_t tree = (size_t)v.T * 8, per_entry = 4 * ((v.hist_tok ? 1 : 0) + (v.bias_tok ? 1 : 0));
@@ -726,7 +731,7 @@ bool plan_walk_table(WalkArgs &a, int log_ctas, size_t &smem) {
     const bool hashed = cap * (per_entry + 4) < part * per_entry;
     if (!hashed) cap = part;
     smem = tree + (size_t)cap * (per_entry + (hashed ? 4 : 0)) + (size_t)part / 8 + (size_t)listed * 4;
-    if (smem > kMost) return false;
+    if (smem > kWalkMostSmem) return false;
     a.cap = (int)cap;
     a.hashed = hashed;
     a.max_list = (int)listed;
@@ -753,7 +758,7 @@ int spec_tree_plan(const int32_t *cand_tok, const int32_t *last_tok, const int32
         return SPEC_ERR_SHAPE;
     const PlanSmem lay = plan_smem(K, n, T);
     if (lay.total > 40 * 1024)
-        SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lay.total));
+        SPEC_CUDA_TRY(cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlanMostSmem));
     int threads = K * n > T * ((T + 31) / 32) ? K * n : T * ((T + 31) / 32);     // words of the masks are the most to write
     threads = threads >= kPlanMaxThreads ? kPlanMaxThreads : (threads + 31) / 32 * 32;
     SPEC_CUDA_TRY(launch_pdl(tree_plan_kernel, dim3(B), dim3(threads), (size_t)lay.total, (cudaStream_t)cuda_stream, cand_tok,

@@ -380,3 +380,41 @@ def test_marshalling_leaves_what_is_wrong_to_the_checks(spec):
         args = {**dict(k=kv, v=kv, k_cache=cache, v_cache=cache, path=z(1, 3), accept_len=z(1), slots=z(1, 3, dt=torch.int64)), **bad}
         with pytest.raises(ValueError):
             spec.spec_kv_commit(**args)
+
+
+def test_host_threads_call_with_different_sizes(spec):
+    """Small and large tables in shared memory in turn, from several host threads at once."""
+    import threading
+    rng = np.random.default_rng(8)
+    large = gpu(ref.random_candidates(rng, 1, 4096, 2, 50)), gpu([3], torch.int32), gpu([4], torch.int32)
+    middle = gpu(ref.random_candidates(rng, 1, 700, 8, 9)), gpu([3], torch.int32), gpu([4], torch.int32)
+    V = 300000
+    logits = torch.zeros(1, 1, V, dtype=torch.bfloat16, device="cuda")
+    node = gpu([[5]], torch.int32), gpu([[-1]], torch.int32), gpu([1], torch.int32)
+    long, short = (gpu(rng.integers(0, V, (1, m)), torch.int32) for m in (9000, 40))
+    size = lambda h: gpu([h.shape[1]], torch.int32)
+    sizes = {long: size(long), short: size(short)}
+    walk = lambda h: spec.spec_verify_tree(*node, logits, 1, hist_tok=h, hist_len=sizes[h])
+    jobs = [lambda: spec.spec_tree_plan(*large, 64), lambda: spec.spec_tree_plan(*middle, 64), lambda: walk(long),
+            lambda: walk(short)]
+    want = [[t.clone() for t in job()] for job in jobs]
+    torch.cuda.synchronize()
+    wrong, start = [], threading.Barrier(len(jobs))
+
+    def work(job, expected):
+        try:
+            start.wait()
+            for _ in range(300):
+                got = job()
+            torch.cuda.current_stream().synchronize()
+            if not all(torch.equal(g, w) for g, w in zip(got, expected)):
+                wrong.append("values")
+        except Exception as e:                                        # noqa: BLE001
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(jobs, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
