@@ -284,10 +284,17 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_sync() {
+__device__ __forceinline__ void cluster_arrive() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    cluster_arrive();
+    cluster_wait();
 }
 __device__ __forceinline__ void store_peer(const void *p, uint32_t rank, float x, int y) {
     uint32_t a;
@@ -525,6 +532,7 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
     __shared__ uint4 keep[kDtype == SPEC_F32 ? 1 : 256];
     __shared__ int child[3], n_list;                     // child: of three steps in turn, so that none is cleared while it is read
     griddep_launch();
+    cluster_arrive();                        // (waited for before the walk: a CTA's shared memory is there once it has begun)
     griddep_wait();
     const spec_tree_verify_t &v = a.v;
     const int t = threadIdx.x, lane = t & 31, ranks = 1 << a.log_ctas;
@@ -594,6 +602,7 @@ __global__ void __launch_bounds__(kWalkThreads, kWalkCtasPerSm) tree_walk_kernel
         }
     }
     __syncthreads();
+    cluster_wait();
 
     int cur = 0, accepted = 0, token = -1;
     if (nodes > 0) {
