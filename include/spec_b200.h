@@ -422,7 +422,8 @@ int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace
  *   path         dev int32 [B, n + 1] (out)   nodes of the path, path[.., 0] = 0; -1 behind it
  * Limits: T <= SPEC_MAX_TREE_NODES; the tokens that penalties and biases touch have to fit a table of 200 KB per CTA, which
  * holds any for V up to 390000 (270000 with penalties and biases), and histories of 10000 tokens for V of millions; else
- * SPEC_ERR_SHAPE.  List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 gets accept_len 0 and -1 elsewhere. */
+ * SPEC_ERR_SHAPE.  List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 (an idle row of the
+ * batch) gets accept_len 0 and -1 elsewhere: spec_kv_commit leaves it as it is, spec_next_ctx would report its last_node. */
 typedef struct {
     int32_t logits_dtype, B, T, V, n, max_hist, max_bias;
     const int32_t *tok, *parent, *n_nodes;
@@ -441,14 +442,16 @@ int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
 /* ---- spec_kv_commit: the accepted path's keys and values
  *     k_cache[l, page, offset] = k[l, b, path[b, j]],  v likewise,  for j = 0 .. accept_len[b], slots[b, j] = (page, offset)
  *     new_len[b] = seq_len[b] + accept_len[b] + 1
- * for all L layers in one launch (k, v must not overlap the caches; of equal slots any row may stay).  16-bit elements of any type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
+ * for all L layers in one launch (k, v must not overlap the caches; of equal slots any row may stay).  16-bit elements of any
+ * type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
  *   k, v         dev [L, B, T, H, D], strides (layer, sequence, node, head)
  *   k_cache, v_cache  dev [L, n_pages, page_size, H, D], strides (layer, page, token, head)
  *   path         dev int32 [B, n + 1], accept_len dev int32 [B]   as spec_verify_tree writes them
  *   slots        dev int64 [B, n + 1]   as spec_page_tables writes them for max_new = n + 1
  *   seq_len, new_len  dev int32 [B]; new_len may be seq_len, or NULL
- * Caches of more than 2^31 - 1 tokens a layer: SPEC_ERR_SHAPE.  accept_len beyond n is taken as n, below 0 nothing is copied.  A node outside [0, T) or a slot outside the cache is not copied, and
- * err_word receives SPEC_ERR_INDEX_RANGE. */
+ * Caches of more than 2^31 - 1 tokens a layer: SPEC_ERR_SHAPE.  accept_len beyond n is taken as n.  Where it is below 0, or path
+ * begins with a negative node (a sequence without nodes), nothing is copied and new_len is seq_len.  Any other node outside
+ * [0, T) or a slot outside the cache is not copied, and err_word receives SPEC_ERR_INDEX_RANGE. */
 typedef struct {
     int32_t L, B, T, n, H, D, page_size, n_pages;
     const void *k, *v;

@@ -678,8 +678,9 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv
     griddep_launch();
     griddep_wait();
     const int b = blockIdx.y, n1 = c.n + 1;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && c.new_len != nullptr)
-        c.new_len[b] = c.seq_len[b] + min(max(c.accept_len[b], -1), c.n) + 1;
+    // (a path that does not begin: a sequence without a node)
+    const int rows = c.path[(size_t)b * n1] < 0 ? 0 : min(max(c.accept_len[b], -1), c.n) + 1;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && c.new_len != nullptr) c.new_len[b] = c.seq_len[b] + rows;
     const int per_head = c.D / 8, per_row = c.H * per_head;
     const long long i = (long long)blockIdx.x * kCommitThreads + threadIdx.x;
     if (i >= 2ll * c.L * per_row) return;
@@ -689,7 +690,6 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv
     const int64_t *ss = is_v ? c.v_stride : c.k_stride, *ds = is_v ? c.vc_stride : c.kc_stride;
     const uint16_t *src = (const uint16_t *)(is_v ? c.v : c.k) + layer * ss[0] + b * ss[1] + head * ss[3] + d;
     uint16_t *dst = (uint16_t *)(is_v ? c.v_cache : c.k_cache) + layer * ds[0] + head * ds[3] + d;
-    const int rows = min(c.accept_len[b], c.n) + 1;
     for (int j0 = 0; j0 < rows; j0 += kCommitRows) {
         uint4 x[kCommitRows];
         uint16_t *to[kCommitRows];

@@ -306,6 +306,27 @@ def test_kv_commit_skips_what_is_out_of_range(spec):
     assert new_len.tolist() == [3] * B and spec.spec_poll_error(err) == spec.SPEC_ERR_INDEX_RANGE
 
 
+def test_an_idle_row_of_the_batch_is_left_as_it_is(spec):
+    B, T, n, V = 3, 2, 1, 40
+    tok, parent, nodes = gpu([[1, 2]] * B, torch.int32), gpu([[-1, 0]] * B, torch.int32), gpu([2, 0, 1], torch.int32)
+    logits = torch.zeros(B, T, V, device="cuda")
+    logits[:, 0, 2] = logits[:, 1, 7] = 1
+    accept, last, nxt, path = spec.spec_verify_tree(tok, parent, nodes, logits, n)
+    assert accept.tolist() == [1, 0, 0] and path.tolist() == [[0, 1], [-1, -1], [0, -1]] and nxt.tolist() == [7, -1, 2]
+    lens, held, count = gpu([3, 5, 4], torch.int32), gpu([1, 2, 1], torch.int32), gpu([5], torch.int32)
+    table = gpu([[0, -1], [1, 2], [3, -1]], torch.int32)
+    slots = spec.spec_page_tables(lens, gpu([2, 0, 2], torch.int32), table, held, gpu([4, 5, 6, 7, 8], torch.int32), count, 4, n + 1)
+    assert slots.tolist() == [[3, 32], [-1, -1], [28, 29]]
+    k = torch.arange(B * T * 8, dtype=torch.float16, device="cuda").reshape(1, B, T, 1, 8)
+    caches = [torch.full((1, 9, 4, 1, 8), -1, dtype=torch.float16, device="cuda") for _ in range(2)]
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    spec.spec_kv_commit(k, k, *caches, path, accept, slots, lens, new_len=lens, err_workspace=err)
+    want = torch.full((36, 8), -1, dtype=torch.float16, device="cuda")
+    want[3], want[32], want[28] = k[0, 0, 0, 0], k[0, 0, 1, 0], k[0, 2, 0, 0]
+    assert all(torch.equal(c.view(36, 8), want) for c in caches)
+    assert lens.tolist() == [5, 5, 5] and spec.spec_poll_error(err) == 0
+
+
 # ---- marshalling ---------------------------------------------------------------------------------------------------
 def test_both_ways_of_marshalling_give_the_same(spec, monkeypatch):
     if spec._pycall is None:
