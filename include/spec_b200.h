@@ -385,7 +385,8 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
  *                overlap on the GPU need workspaces of their own.  `out` and `lse` must not overlap the inputs.
  * Limits: D a multiple of 8, at most 128; Hq a multiple of Hkv; T <= SPEC_MAX_TREE_NODES; else SPEC_ERR_SHAPE.
  * Lengths out of [0, max_pages * page_size] and node counts out of [0, T] are clamped, a page id outside [0, n_pages) reads as
- * zeros, and err_word receives SPEC_ERR_INDEX_RANGE. */
+ * zeros, and err_word receives SPEC_ERR_INDEX_RANGE.  A copy or a product that does not end within a second (SPEC_ERR_TIMEOUT) leaves
+ * out undefined. */
 typedef struct {
     int32_t dtype, B, T, Hq, Hkv, D;
     int32_t page_size, n_pages, max_pages;
