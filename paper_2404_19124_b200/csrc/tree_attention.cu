@@ -24,10 +24,10 @@
 // busy, nor the exponentials, 39 %, were the limit, but the way round.)  Units of more than 128 rows have a stream per 128
 // rows, which take both halves of every tile of keys; in smaller ones each stream takes a half, and the two results are joined.
 //
-// What bounds it.  Up to 128 rows per key head, the keys' way from HBM: 131072 tokens of one sequence 113 to 118 us, 4.6 TB/s of
-// 6.5; 16 sequences with 40 key heads and trees of 31 to 61 nodes 111 us, 3.7 TB/s (units of 10 tiles, whose ends nothing hides).
+// What bounds it.  Up to 128 rows per key head, the keys' way from HBM: 131072 tokens of one sequence 113 to 120 us, 4.6 TB/s of
+// 6.5; 16 sequences with 40 key heads and trees of 31 to 61 nodes 111 to 120 us, 3.6 TB/s (units of 10 tiles, whose ends nothing hides).
 // With more rows the chain scores - softmax - products of a step and the power cap: 64 sequences, trees of 65 to 129 nodes,
-// four query heads per key head 368 us from a cool start, 400 to 420 on and on (1.6 GHz), 0.55 of 1.63 PFLOP/s.  Few tiles:
+// four query heads per key head 368 us from a cool start, 400 to 460 on and on (1.6 GHz), 0.55 of 1.63 PFLOP/s.  Few tiles:
 // latency, 20 us for single tokens of 4 sequences, of which the second kernel is 4.
 #include <limits.h>
 #include <math.h>

@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(const TableArg
 // shared memory, and marks them in a bitmap: the pass over the row leaves them out (and what the grammar forbids), and every
 // listed token is looked at by itself.  The table is hashed while that is smaller, which lets four CTAs share an SM for
 // histories of a few thousand tokens, else it has an entry per token.  64 sequences, a vocabulary of 128256, histories of up to
-// 2048 tokens, a grammar: 54 us (34 without constraints); a table of 130 KB and checks per element took 278.
+// 2048 tokens, a grammar: 53 us (34 without constraints); a table of 130 KB and checks per element took 278.
 constexpr int kWalkThreads = 256;
 constexpr int kWalkWarps = kWalkThreads / 32;
 constexpr int kWalkCtasPerSm = 4;            // by registers
