@@ -445,9 +445,11 @@ __device__ __forceinline__ void blank(uint4 &x, uint32_t use, const uint4 *keep)
 }
 
 // The maximum over this CTA's blocks of a row, of the tokens that `allow` (null: all) and `marked` (null: none) leave.  A thread's
-// vectors rise and four of them (and the grammar's bits) are in flight.  It keeps the vector with the greatest maximum, without a
+// vectors rise and four of them (and the grammar's bits) are in flight.  It keeps the first vector with the greatest maximum, without a
 // branch, and looks for the element at the end: a branch for every new maximum is taken by some lane nearly always.
-// kAligned: the row begins at a vector, so that no vector holds elements of two blocks or two bytes of bits.
+// kAligned: the row begins at a vector, so that no vector holds elements of two blocks or two bytes of bits.  Otherwise the vectors
+// in which blocks end come last and may lie before the one that the thread has kept: equal maxima are told apart by their place (and a
+// vector that two blocks share is the first one's end).
 template <int kDtype, bool kAligned>
 __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uint32_t rank, const uint32_t *allow, int words,
                                          const uint32_t *marked, const uint4 *keep, Best &best) {
@@ -463,7 +465,8 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
     uint32_t best_use = 0;
     int best_e0 = 0;
     auto first_of = [&](int turn) { return ((turn << a.log_ctas) + (int)rank) * kBlockTokens; };
-    auto look = [&](uint4 x, int e0, int begin, int turn, uint32_t use) {        // use: the grammar's bits from max(e0, begin) on
+    // use: the grammar's bits from max(e0, begin) on; ends: a vector in which a block ends
+    auto look = [&](uint4 x, int e0, int begin, int turn, uint32_t use, bool ends) {
         const int from = kAligned ? e0 : max(e0, begin);
         if (marked != nullptr) use &= ~bits_from<kAligned>(marked, turn * kBlockTokens + from - begin, a.part / 8);
         use = use << (from - e0) & kAll;
@@ -481,7 +484,7 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
         }
         if (use != kAll) blank<kDtype>(x, use, keep);
         const float top = fmaxf(Logit<kDtype>::most(x), -INFINITY);
-        const bool take = use != 0 && (best_use == 0 || top > best_top);
+        const bool take = use != 0 && (best_use == 0 || top > best_top || (ends && top == best_top && e0 <= best_e0));
         best_top = take ? top : best_top;
         best_use = take ? use : best_use;
         best_e0 = take ? e0 : best_e0;
@@ -507,7 +510,7 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
         for (int k = 0; k < kAhead; ++k) {
             const int turn = turn0 + k / kPerThread, begin = first_of(turn);
             const int e0 = begin - skew + ((int)threadIdx.x + k % kPerThread * kWalkThreads) * kPer;
-            if (turn < turns && e0 < V) look(x[k], e0, begin, turn, use[k]);
+            if (turn < turns && e0 < V) look(x[k], e0, begin, turn, use[k], false);
         }
     }
     if (!kAligned)                                       // the vectors in which blocks end
@@ -516,7 +519,7 @@ __device__ __forceinline__ void scan_row(const WalkArgs &a, const char *row, uin
             if (e0 >= V) continue;
             const uint4 x = e0 + kPer <= V ? __ldg((const uint4 *)((const char *)vec + (long long)(e0 + skew) * Logit<kDtype>::kBytes))
                                            : make_uint4(0, 0, 0, 0);
-            look(x, e0, begin, turn, allow != nullptr ? bits_from<kAligned>(allow, e0, words * 4) : kAll);
+            look(x, e0, begin, turn, allow != nullptr ? bits_from<kAligned>(allow, e0, words * 4) : kAll, true);
         }
     if (best_use == 0) return;
 #pragma unroll
