@@ -185,15 +185,14 @@ __device__ __forceinline__ int in_range(int x, int lo, int hi, int32_t *err) {
 // The slot of new token j of a sequence that has `held` pages.
 __device__ __forceinline__ int64_t slot_of(const TableArgs &a, int b, int j) {
     const int length = max(a.seq_len[b], 0), fresh = a.n_new == nullptr ? a.max_new : min(a.n_new[b], a.max_new);
-    const long long at = (long long)length + j;
-    const int page = (int)(at / a.page);
-    if (j >= fresh || page >= a.n_pages_out[b]) return -1;
+    const unsigned at = (unsigned)length + (unsigned)j, page = at / (unsigned)a.page;        // both below 2^31: the sum fits
+    if (j >= fresh || page >= (unsigned)a.n_pages_out[b]) return -1;
     const int id = a.table[b * a.stride + page];
     if (id < 0) {
         report_error(a.err, SPEC_ERR_INDEX_RANGE);
         return -1;
     }
-    return (int64_t)id * a.page + (at - (long long)page * a.page);
+    return (int64_t)id * a.page + (at - page * (unsigned)a.page);
 }
 
 __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const TableArgs a, int with_slots) {
@@ -793,7 +792,7 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
     const bool one = all <= 4 * kTableThreads;
     SPEC_CUDA_TRY(launch_pdl(page_tables_kernel, dim3(1), dim3(kTableThreads), 0, st, a, one ? 1 : 0));
     if (!one) {
-        const int blocks = (all + kSlotThreads - 1) / kSlotThreads, most = 8 * num_sms();
+        const int blocks = (all - 1) / kSlotThreads + 1, most = 8 * num_sms();
         SPEC_CUDA_TRY(launch_pdl(page_slots_kernel, dim3(blocks < most ? blocks : most), dim3(kSlotThreads), 0, st, a));
     }
     return SPEC_OK;
