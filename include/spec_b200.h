@@ -373,7 +373,8 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
  *     out[b, i, h] = sum softmax(scale * <q[b, i, h], key>) * value,   lse[b, i, h] = log sum exp(scale * <q, key>)
  * A row without any key gets zeros and lse = -inf.  Keys that a row does not see do not touch it, whatever they hold.  Rows
  * i >= n_nodes[b] of out and lse are left as they are.  T = 1 without a mask is a plain decoding step.
- * Scores, softmax statistics and sums are fp32; the probabilities are rounded to `dtype` before they meet the values.
+ * Scores, softmax statistics and sums are fp32; the probabilities are rounded to `dtype` before they meet the values, each by half a
+ * step of it at most, in fp16 by 2^-32 of the row's greatest if that is more.
  *   dtype        SPEC_BF16 or SPEC_F16, of q, k, v, caches and out; 16-byte aligned pointers, strides multiples of 8
  *   q, out       dev [B, T, Hq, D], strides (sequence, node, head);  k, v  dev [B, T, Hkv, D], the same
  *   k_cache, v_cache  dev [n_pages, page_size, Hkv, D], strides (page, token, head): any order of these in memory

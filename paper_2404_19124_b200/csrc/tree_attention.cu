@@ -71,6 +71,11 @@ constexpr int kUnitFlags = 8;
 constexpr uint64_t kWaitMaxNs = 1000000000;     // after which a wait gives up
 constexpr uint32_t kWaitHintNs = 20000;
 constexpr float kRescaleAbove = 8.f;            // see softmax_step
+// Probabilities are 2^kLift times what the maximum gives them.  In fp16, whose least number is 2^-24, those of less than 2^-25 of the
+// maximum would become zero in the products but not in their sum (131071 keys 17.4 below one: 0.36 % of the result's weight lost);
+// this way the border is 2^-32, and the greatest, 2^(kRescaleAbove + 7), is below 65504.
+template <int kDtype>
+constexpr float kLift = kDtype == SPEC_F16 ? 7.f : 0.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -745,7 +750,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 // One step of a row: probabilities in place of the scores.  The maximum follows the steps lazily: probabilities are taken against an
 // older one as long as none exceeds 2^8 of it, which costs no precision in fp32 sums nor in the 16-bit probabilities and
 // saves nearly every pass over the accumulated output (a pass waits for the products of the step before).  The probabilities are
-// rounded to the 16 bits that the tensor cores take beside the values, each by half a step at most; their sum is not.
+// rounded to the 16 bits that the tensor cores take beside the values, each by half a step at most (in fp16 by 2^-32 of the
+// greatest if that is more: see kLift); their sum is not.
 template <int kDtype, int kHalves>
 __device__ __forceinline__ bool softmax_step(const AttnArgs &g, Shared *sh, uint32_t s_addr, uint32_t o_addr, bool first,
                                              uint64_t *pv_done, uint32_t pv_parity, bool masked, uint64_t seen, Row &row) {
@@ -784,7 +790,7 @@ __device__ __forceinline__ bool softmax_step(const AttnArgs &g, Shared *sh, uint
             tmem_st16(o_addr + c * 16, r);
         }
     }
-    const float base = row.top == -INFINITY ? 0.f : row.top;
+    const float base = row.top == -INFINITY ? 0.f : row.top - kLift<kDtype>;
     const float2 scale = make_float2(g.scale_log2, g.scale_log2), minus = make_float2(-base, -base);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -869,6 +875,7 @@ __device__ bool softmax_role(const AttnArgs &g, Shared *sh) {
         }
         // (A buffer's products are done when its next scores are there, so that this phase is the current one or the last.)
         if (!warp_wait(&sh->pv_done[stream][(count - 1) & 1], (count - 1) >> 1 & 1, sh, a.err_word)) return false;
+        row.top -= kLift<kDtype>;                        // what the exponents were taken against
         // the two streams of one query tile are joined: each warp group takes every other 32 columns
         float w[2] = {1.f, 0.f};
         if (!two) {
