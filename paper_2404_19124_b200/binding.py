@@ -567,10 +567,10 @@ def spec_page_tables(seq_len: torch.Tensor, n_new: Optional[torch.Tensor], block
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Grows block_table [B, max_pages] for seq_len + n_new tokens (n_new None: max_new everywhere) from the end of free_pages;
     returns slots, int64 [B, max_new].  n_pages [B] and free_count [1] are updated in place unless outputs for them are given."""
-    if _pycall is not None and slots is not None and err_workspace is None and max_new is None:
+    if _pycall is not None and slots is not None and max_new is None:
         status = _pycall.page_tables(seq_len, n_new, block_table, n_pages, free_pages, free_count, page_size, slots,
                                      n_pages if n_pages_out is None else n_pages_out,
-                                     free_count if free_count_out is None else free_count_out, stream)
+                                     free_count if free_count_out is None else free_count_out, err_workspace, stream)
         if status is not None:
             if status != SPEC_OK:
                 raise SpecError(status, "spec_page_tables")
@@ -616,9 +616,9 @@ def spec_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cac
     """q [B, T, Hq, D] over the cache [pages, page_size, Hkv, D] (any strides but a dense last dimension; a cache kept as
     [pages, Hkv, page_size, D] is passed transposed) and the tree's own k, v [B, T, Hkv, D].  mask: SpecTree.mask, None for
     chains; scale: D ** -0.5 by default.  Returns out; lse (fp32 [B, T, Hq]) is written when given."""
-    if _pycall is not None and out is not None and workspace is not None and err_workspace is None:
+    if _pycall is not None and out is not None and workspace is not None:
         status = _pycall.tree_attention(q, k, v, k_cache, v_cache, block_table, seq_len, mask, n_nodes,
-                                        q.shape[-1] ** -0.5 if scale is None else scale, out, lse, workspace, stream)
+                                        q.shape[-1] ** -0.5 if scale is None else scale, out, lse, workspace, err_workspace, stream)
         if status is not None:
             if status != SPEC_OK:
                 raise SpecError(status, "spec_tree_attention")
@@ -708,8 +708,8 @@ def spec_kv_commit(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
                    stream: Optional[torch.cuda.Stream] = None) -> None:
     """Copies the accepted path's rows of k, v [L, B, T, H, D] to the slots [B, n + 1] of the caches [L, pages, page_size, H, D];
     new_len (may be seq_len) receives seq_len + accept_len + 1."""
-    if _pycall is not None and err_workspace is None:
-        status = _pycall.kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, stream)
+    if _pycall is not None:
+        status = _pycall.kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, err_workspace, stream)
         if status is not None:
             if status != SPEC_OK:
                 raise SpecError(status, "spec_kv_commit")

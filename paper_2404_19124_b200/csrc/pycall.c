@@ -244,7 +244,22 @@ static int strided(PyObject *t, PyObject *dtype, long long dev, int nd, const lo
     return !PyErr_Occurred();
 }
 
-/* the stream object's device is left to the Python checks, and so is an error word */
+/* An int32 word on device `dev` in a tensor of any type, or None: a null pointer. */
+static int error_word(PyObject *t, long long dev, int32_t **err) {
+    uintptr_t p = 0;
+    long long n, on, size;
+    PyObject *o;
+    if (t != Py_None) {
+        if (!bytes_of(t, &p, &n) || !number(t, s_get_device, &on) || on != dev || p % 4 || !(o = PyObject_GetAttr(t, s_itemsize))) return 0;
+        size = PyLong_AsLongLong(o);
+        Py_DECREF(o);
+        if (PyErr_Occurred() || n * size < 4) return 0;
+    }
+    *err = (int32_t *)p;
+    return 1;
+}
+
+/* the stream object's device is left to the Python checks */
 static int own_stream(PyObject *stream, uintptr_t *st) { return stream == Py_None && stream_of(stream, st); }
 
 /* tree_plan(cand_tok, last_tok, seq_len, T, tok, pos, parent, mask, node_of, n_nodes, stream) -> status or None */
@@ -271,31 +286,33 @@ static PyObject *py_tree_plan(PyObject *self, PyObject *const *a, Py_ssize_t n) 
     return PyLong_FromLong(status);
 }
 
-/* page_tables(seq_len, n_new, block_table, n_pages, free_pages, free_count, page_size, slots, n_pages_out, free_count_out, stream) */
+/* page_tables(seq_len, n_new, block_table, n_pages, free_pages, free_count, page_size, slots, n_pages_out, free_count_out, err_workspace,
+ * stream) */
 static PyObject *py_page_tables(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     long long b[1], t[2], f[1], s[2], dev, on;
     int64_t stride[1], *ps;
     uintptr_t pl, pslots, pf, st;
-    int32_t *fresh, *table, *held, *count, *held_out, *count_out;
+    int32_t *fresh, *table, *held, *count, *held_out, *count_out, *err;
     int status;
-    if (n != 11 || !current(&dev) || !look(a[0], t_i32, 1, b, &pl, NULL) || !number(a[0], s_get_device, &on) || on != dev ||
+    if (n != 12 || !current(&dev) || !look(a[0], t_i32, 1, b, &pl, NULL) || !number(a[0], s_get_device, &on) || on != dev ||
         !vector(a[1], t_i32, dev, b[0], 1, &fresh) || !strided(a[2], t_i32, dev, 2, NULL, 1, t, stride, &table) || t[0] != b[0] ||
         !vector(a[3], t_i32, dev, b[0], 0, &held) || !look(a[4], t_i32, 1, f, &pf, NULL) || !number(a[4], s_get_device, &on) ||
         on != dev || !vector(a[5], t_i32, dev, 1, 0, &count) || !look(a[7], t_i64, 2, s, &pslots, NULL) ||
         !number(a[7], s_get_device, &on) || on != dev || s[0] != b[0] || !vector(a[8], t_i32, dev, b[0], 0, &held_out) ||
-        !vector(a[9], t_i32, dev, 1, 0, &count_out) || !own_stream(a[10], &st))
+        !vector(a[9], t_i32, dev, 1, 0, &count_out) || !error_word(a[10], dev, &err) || !own_stream(a[11], &st))
         return unusual();
     const long long page = PyLong_AsLongLong(a[6]);
     if (PyErr_Occurred() || page < 1 || page > INT32_MAX) return unusual();
     ps = (int64_t *)pslots;
     Py_BEGIN_ALLOW_THREADS
     status = f_tables((const int32_t *)pl, fresh, (int)b[0], (int)page, (int)s[1], table, stride[0] ? stride[0] : t[1], (int)t[1],
-                      held, (const int32_t *)pf, count, (int)f[0], ps, held_out, count_out, NULL, (void *)st);
+                      held, (const int32_t *)pf, count, (int)f[0], ps, held_out, count_out, err, (void *)st);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
 }
 
-/* tree_attention(q, k, v, k_cache, v_cache, block_table, seq_len, mask, n_nodes, scale, out, lse, workspace, stream) */
+/* tree_attention(q, k, v, k_cache, v_cache, block_table, seq_len, mask, n_nodes, scale, out, lse, workspace, err_workspace,
+ * stream) */
 static PyObject *py_tree_attention(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     spec_tree_attention_t x;
     long long q[4], d[4], c[4], t[2], dev, on, wn;
@@ -304,7 +321,7 @@ static PyObject *py_tree_attention(PyObject *self, PyObject *const *a, Py_ssize_
     PyObject *dtype;
     int status;
     memset(&x, 0, sizeof x);
-    if (n != 14 || !current(&dev) || !(dtype = PyObject_GetAttr(a[0], s_dtype))) return unusual();
+    if (n != 15 || !current(&dev) || !(dtype = PyObject_GetAttr(a[0], s_dtype))) return unusual();
     Py_DECREF(dtype);                                   /* the dtype objects live as long as torch */
     if (dtype != t_bf16 && dtype != t_f16) return unusual();
     x.dtype = dtype == t_bf16 ? SPEC_BF16 : SPEC_F16;
@@ -327,7 +344,7 @@ static PyObject *py_tree_attention(PyObject *self, PyObject *const *a, Py_ssize_
     wn *= PyLong_AsLongLong(size);
     Py_DECREF(size);
     x.scale = (float)PyFloat_AsDouble(a[9]);
-    if (PyErr_Occurred() || !own_stream(a[13], &st)) return unusual();
+    if (PyErr_Occurred() || !error_word(a[13], dev, &x.err_word) || !own_stream(a[14], &st)) return unusual();
     x.B = (int)q[0], x.T = (int)q[1], x.Hq = (int)q[2], x.D = (int)q[3], x.Hkv = (int)kv[2];
     x.n_pages = (int)cache[0], x.page_size = (int)cache[1], x.max_pages = (int)t[1];
     x.table_stride = q[0] > 1 ? ts[0] : t[1];
@@ -381,7 +398,7 @@ static PyObject *py_verify_tree(PyObject *self, PyObject *const *a, Py_ssize_t n
     return PyLong_FromLong(status);
 }
 
-/* kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, stream) */
+/* kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, err_workspace, stream) */
 static PyObject *py_kv_commit(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     spec_kv_commit_t x;
     long long k[5], c[5], d[5], p[2], dev;
@@ -389,7 +406,7 @@ static PyObject *py_kv_commit(PyObject *self, PyObject *const *a, Py_ssize_t n) 
     PyObject *dtype;
     int status;
     memset(&x, 0, sizeof x);
-    if (n != 10 || !current(&dev) || !(dtype = PyObject_GetAttr(a[0], s_dtype))) return unusual();
+    if (n != 11 || !current(&dev) || !(dtype = PyObject_GetAttr(a[0], s_dtype))) return unusual();
     Py_DECREF(dtype);
     if (dtype != t_bf16 && dtype != t_f16) return unusual();
     if (!strided(a[0], dtype, dev, 5, NULL, 0, k, x.k_stride, &x.k) || !strided(a[1], dtype, dev, 5, k, 0, d, x.v_stride, &x.v) ||
@@ -397,7 +414,7 @@ static PyObject *py_kv_commit(PyObject *self, PyObject *const *a, Py_ssize_t n) 
         !strided(a[3], dtype, dev, 5, c, 1, d, x.vc_stride, &x.v_cache) || !look(a[4], t_i32, 2, p, &at, NULL) || p[0] != k[1] ||
         !dense(a[4], t_i32, dev, 2, p, 0, &x.path) || !vector(a[5], t_i32, dev, k[1], 0, &x.accept_len) ||
         !dense(a[6], t_i64, dev, 2, p, 0, &x.slots) || !vector(a[7], t_i32, dev, k[1], 1, &x.seq_len) ||
-        !vector(a[8], t_i32, dev, k[1], 1, &x.new_len) || !own_stream(a[9], &st))
+        !vector(a[8], t_i32, dev, k[1], 1, &x.new_len) || !error_word(a[9], dev, &x.err_word) || !own_stream(a[10], &st))
         return unusual();
     x.L = (int)k[0], x.B = (int)k[1], x.T = (int)k[2], x.n = (int)p[1] - 1, x.H = (int)k[3], x.D = (int)k[4];
     x.n_pages = (int)c[1], x.page_size = (int)c[2];

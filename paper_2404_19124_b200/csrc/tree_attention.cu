@@ -1171,6 +1171,7 @@ int spec_tree_attention(const spec_tree_attention_t *a, void *workspace, size_t 
     const void *ptrs[] = {a->q, a->k, a->v, a->k_cache, a->v_cache, a->out};
     for (const void *p : ptrs)
         if ((uintptr_t)p % 16 != 0) return SPEC_ERR_INVALID_ARG;
+    if ((uintptr_t)a->err_word % 4 != 0) return SPEC_ERR_INVALID_ARG;
     if (!strides_ok(a->q_stride) || !strides_ok(a->k_stride) || !strides_ok(a->v_stride) || !strides_ok(a->kc_stride) ||
         !strides_ok(a->vc_stride) || !strides_ok(a->out_stride))
         return SPEC_ERR_SHAPE;

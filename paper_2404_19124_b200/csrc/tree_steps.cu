@@ -784,6 +784,7 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
     if (!seq_len || !block_table || !n_pages || !free_pages || !free_count || !slots || !n_pages_out || !free_count_out)
         return SPEC_ERR_INVALID_ARG;
     if (B <= 0 || page_size <= 0 || max_new <= 0 || max_pages <= 0 || n_free <= 0) return SPEC_ERR_INVALID_ARG;
+    if ((uintptr_t)err_word % 4 != 0) return SPEC_ERR_INVALID_ARG;
     if (table_stride < max_pages || (long long)B * max_new > INT_MAX || (long long)B * max_pages > INT_MAX) return SPEC_ERR_SHAPE;
     const TableArgs a = {seq_len, n_new, B, page_size, max_new, block_table, table_stride, max_pages, n_pages, free_pages,
                          free_count, n_free, slots, n_pages_out, free_count_out, err_word};
@@ -834,7 +835,7 @@ int spec_verify_tree(const spec_tree_verify_t *v, void *cuda_stream) {
 
 int spec_kv_commit(const spec_kv_commit_t *c, void *cuda_stream) {
     if (!c || !c->k || !c->v || !c->k_cache || !c->v_cache || !c->path || !c->accept_len || !c->slots) return SPEC_ERR_INVALID_ARG;
-    if (c->new_len && !c->seq_len) return SPEC_ERR_INVALID_ARG;
+    if ((c->new_len && !c->seq_len) || (uintptr_t)c->err_word % 4 != 0) return SPEC_ERR_INVALID_ARG;
     if (c->L <= 0 || c->B <= 0 || c->T <= 0 || c->n < 0 || c->H <= 0 || c->D <= 0 || c->page_size <= 0 || c->n_pages <= 0)
         return SPEC_ERR_INVALID_ARG;
     if (c->D % 8 != 0 || c->B > 65535 || (long long)c->L * c->H * c->D > INT_MAX / 4) return SPEC_ERR_SHAPE;
