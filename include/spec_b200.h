@@ -443,7 +443,7 @@ int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
 
 /* ---- spec_kv_commit: the accepted path's keys and values
  *     k_cache[l, page, offset] = k[l, b, path[b, j]],  v likewise,  for j = 0 .. accept_len[b], slots[b, j] = (page, offset)
- *     new_len[b] = seq_len[b] + accept_len[b] + 1
+ *     new_len[b] = seq_len[b] + accept_len[b] + 1 - (accepted tokens behind the last one that has a slot)
  * for all L layers in one launch (k, v must not overlap the caches; of equal slots any row may stay).  16-bit elements of any
  * type; 16-byte aligned pointers, strides multiples of 8, D a multiple of 8.
  *   k, v         dev [L, B, T, H, D], strides (layer, sequence, node, head)
@@ -453,7 +453,9 @@ int spec_verify_tree(const spec_tree_verify_t *v /*host*/, void *cuda_stream);
  *   seq_len, new_len  dev int32 [B]; new_len may be seq_len, or NULL
  * Caches of more than 2^31 - 1 tokens a layer: SPEC_ERR_SHAPE.  accept_len beyond n is taken as n.  Where it is below 0, or path
  * begins with a negative node (a sequence without nodes), nothing is copied and new_len is seq_len.  Any other node outside
- * [0, T) or a slot outside the cache is not copied, and err_word receives SPEC_ERR_INDEX_RANGE. */
+ * [0, T) or a slot outside the cache is not copied, and err_word receives SPEC_ERR_INDEX_RANGE.  Where pages ran out the slots of a
+ * sequence end in -1 (see spec_page_tables): its length stops with them, and the keys and values of the tokens behind it have to
+ * be computed again once there are pages.  (An index out of range before a good one does not shorten it.) */
 typedef struct {
     int32_t L, B, T, n, H, D, page_size, n_pages;
     const void *k, *v;

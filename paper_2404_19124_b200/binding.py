@@ -707,7 +707,7 @@ def spec_kv_commit(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
                    new_len: Optional[torch.Tensor] = None, err_workspace: Optional[torch.Tensor] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> None:
     """Copies the accepted path's rows of k, v [L, B, T, H, D] to the slots [B, n + 1] of the caches [L, pages, page_size, H, D];
-    new_len (may be seq_len) receives seq_len + accept_len + 1."""
+    new_len (may be seq_len) receives seq_len + accept_len + 1, less the accepted tokens behind the last one that has a slot."""
     if _pycall is not None:
         status = _pycall.kv_commit(k, v, k_cache, v_cache, path, accept_len, slots, seq_len, new_len, err_workspace, stream)
         if status is not None:

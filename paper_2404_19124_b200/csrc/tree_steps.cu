@@ -682,7 +682,11 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const spec_kv
     const int b = blockIdx.y, n1 = c.n + 1;
     // (a path that does not begin: a sequence without a node)
     const int rows = c.path[(size_t)b * n1] < 0 ? 0 : min(max(c.accept_len[b], -1), c.n) + 1;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && c.new_len != nullptr) c.new_len[b] = c.seq_len[b] + rows;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && c.new_len != nullptr) {
+        int stored = rows;                   // a length counts no tokens behind the last slot: there are none where pages ran out
+        while (stored > 0 && c.slots[(size_t)b * n1 + stored - 1] == -1) --stored;
+        c.new_len[b] = c.seq_len[b] + stored;
+    }
     const int per_head = c.D / 8, per_row = c.H * per_head;
     const long long i = (long long)blockIdx.x * kCommitThreads + threadIdx.x;
     if (i >= 2ll * c.L * per_row) return;

@@ -87,3 +87,43 @@ def test_error_words_that_are_none_are_refused(spec):
         for call in (calls.tables, calls.attention, calls.commit):
             with pytest.raises(ValueError, match="err_workspace"):
                 call(err)
+
+
+# ---- lengths after a shortage of pages ------------------------------------------------------------------------------
+def test_a_commit_counts_the_rows_that_have_a_slot(spec):
+    """Sequences that get all, some or none of their pages: the new length ends where their slots end."""
+    B, n, page, pages, D = 5, 4, 4, 16, 8
+    lens, held = i32([6, 6, 8, 3, 7]), i32([2, 2, 2, 1, 2])
+    table = torch.full((B, 6), -1, dtype=torch.int32, device="cuda")
+    table[0, :2], table[1, :2], table[2, :2], table[3, :1], table[4, :2] = i32([0, 1]), i32([2, 3]), i32([4, 5]), i32([6]), i32([7, 8])
+    err, count = zeros(1), i32([1])
+    slots = spec.spec_page_tables(lens, None, table, held, i32([9]), count, page, max_new=n + 1, err_workspace=err)
+    assert spec.spec_poll_error(err) == spec.SPEC_ERR_PAGES and (slots >= 0).sum(1).tolist() == [5, 2, 0, 1, 1]
+    accept = i32([4, 4, 2, 0, 3])                                     # 5, 5, 3, 1 and 4 rows, for 5, 2, none, 1 and 1 slots
+    path = torch.arange(n + 1, dtype=torch.int32, device="cuda").repeat(B, 1)
+    k = torch.arange(B * (n + 1) * D, dtype=torch.int16, device="cuda").view(1, B, n + 1, 1, D)
+    caches = [torch.full((1, pages, page, 1, D), -1, dtype=torch.int16, device="cuda") for _ in range(2)]
+    new_len, err = zeros(B), zeros(1)
+    spec.spec_kv_commit(k, k, *caches, path, accept, slots, lens, new_len=new_len, err_workspace=err)
+    assert new_len.tolist() == [11, 8, 8, 4, 8] and spec.spec_poll_error(err) == spec.SPEC_ERR_INDEX_RANGE
+    for b in range(B):                                                # every token that a length counts is where the table says
+        for j in range(int(lens[b]), int(new_len[b])):
+            for c in caches:
+                assert torch.equal(c[0, table[b, j // page], j % page, 0], k[0, b, j - int(lens[b]), 0])
+    assert sum(int((c.view(-1, D) >= 0).all(1).sum()) for c in caches) == 2 * (5 + 2 + 0 + 1 + 1)
+
+
+def test_a_commit_in_place_after_a_shortage(spec):
+    """new_len may be seq_len; more sequences than a block has threads, rows of every number."""
+    B, n, page = 700, 3, 4
+    accept = torch.arange(B, device="cuda").remainder(n + 1).to(torch.int32)
+    room = torch.arange(B, device="cuda").remainder(n + 3)            # slots that the sequence has; n + 1 or more: all
+    slots = torch.arange(B * (n + 1), device="cuda").view(B, n + 1)
+    slots[torch.arange(n + 1, device="cuda")[None] >= room[:, None]] = -1
+    path = torch.arange(n + 1, dtype=torch.int32, device="cuda").repeat(B, 1)
+    k = torch.zeros(2, B, n + 1, 1, 8, dtype=torch.bfloat16, device="cuda")
+    cache = torch.ones(2, B * (n + 1) // page, page, 1, 8, dtype=torch.bfloat16, device="cuda")
+    lens = torch.arange(B, dtype=torch.int32, device="cuda")
+    spec.spec_kv_commit(k, k, cache, cache.clone(), path, accept, slots, lens, new_len=lens)
+    want = torch.arange(B, device="cuda") + torch.minimum(accept + 1, room)
+    assert torch.equal(lens.long(), want)
