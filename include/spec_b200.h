@@ -216,10 +216,13 @@ int spec_verify_early(const int32_t *cand_tok, const void *base_logits, int logi
  *   base_state  dev bf16 [B, K, n+1, d_base]  the base model's state vectors at the positions whose
  *                                             logits spec_verify looked at
  *   best_cand, accept_len  dev int32 [B]      as written by spec_verify* earlier on the same stream
- *   ctx_state   dev bf16 [B, d_base] (out)    ctx_state[b,:] = base_state[b, best_cand[b], accept_len[b], :]
+ *   ctx_state   dev bf16 [B, d_base] (out)    ctx_state[b,:] = base_state[b, best_cand[b], accept_len[b], :]; zeros
+ *                                             where an index is out of range
  *   err_word    dev int32, or NULL            receives SPEC_ERR_INDEX_RANGE if it was 0 and an index is
  *                                             out of range (e.g. the word at offset 0 of the verify
- *                                             workspace, which spec_poll_error reads); never cleared here
+ *                                             workspace, which spec_poll_error reads); never cleared here.
+ *                                             best_cand 0 with accept_len -1 is no error: a sequence without
+ *                                             nodes (see spec_verify_tree)
  * Only enqueues one copy kernel on `cuda_stream`; nothing is allocated.  Rows are copied 16 bytes at a
  * time when d_base is a multiple of 8 and both tensors are 16-byte aligned, else element by element. */
 int spec_next_ctx(const void *base_state, const int32_t *best_cand, const int32_t *accept_len, int B, int K, int n,
@@ -327,7 +330,8 @@ int spec_set_head_fp8(spec_handle_t h, int level, const void *q, const float *sc
  *     spec_tree_attention  per layer: the tree's queries attend to the cache and to their ancestors in the tree
  *     spec_verify_tree     the accepted path of the tree by the base model's logits, the next token behind it
  *     spec_kv_commit       the accepted path's keys and values, all layers, go to their slots in the cache
- * then spec_next_ctx on base_state seen as [B, 1, T, d_base] with best_cand = 0 and accept_len = last_node, and spec_draft.
+ * then spec_next_ctx on base_state seen as [B, 1, T, d_base] with best_cand = 0 and accept_len = last_node, and spec_draft with
+ * last_tok = next_tok (any token of the vocabulary where that is -1: an idle sequence, or a grammar that allows nothing).
  * All of them only enqueue kernels on `cuda_stream`, with the device that owns the pointers current.  `err_word` (dev
  * int32, or NULL) receives the first device-side error if it was 0; it is never cleared here, and spec_poll_error
  * reads it.  Strides are in elements; a dimension of size 1 may have stride 0.
@@ -425,7 +429,7 @@ int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace
  * Limits: T <= SPEC_MAX_TREE_NODES; the tokens that penalties and biases touch have to fit a table of 200 KB per CTA, which
  * holds any for V up to 390000 (270000 with penalties and biases), and histories of 10000 tokens for V of millions; else
  * SPEC_ERR_SHAPE.  List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 (an idle row of the
- * batch) gets accept_len 0 and -1 elsewhere: spec_kv_commit leaves it as it is, spec_next_ctx would report its last_node. */
+ * batch) gets accept_len 0 and -1 elsewhere: spec_kv_commit leaves it as it is, spec_next_ctx writes zeros for it. */
 typedef struct {
     int32_t logits_dtype, B, T, V, n, max_hist, max_bias;
     const int32_t *tok, *parent, *n_nodes;

@@ -437,7 +437,8 @@ def spec_next_ctx(base_state: torch.Tensor, best_cand: torch.Tensor, accept_len:
                   ctx_state: Optional[torch.Tensor] = None, err_workspace: Optional[torch.Tensor] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """ctx_state[b] = base_state[b, best_cand[b], accept_len[b]]: the state the next spec_draft starts from.
-    `err_workspace` (e.g. the verify workspace) receives SPEC_ERR_INDEX_RANGE at offset 0 on a bad index."""
+    `err_workspace` (e.g. the verify workspace) receives SPEC_ERR_INDEX_RANGE at offset 0 on a bad index, whose row becomes
+    zeros; so does that of best_cand 0 with accept_len -1, a sequence without nodes, which is no error."""
     if _pycall is not None and ctx_state is not None:
         status = _pycall.next_ctx(base_state, best_cand, accept_len, ctx_state, err_workspace, stream)
         if status is not None:

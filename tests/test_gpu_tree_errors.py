@@ -127,3 +127,32 @@ def test_a_commit_in_place_after_a_shortage(spec):
     spec.spec_kv_commit(k, k, cache, cache.clone(), path, accept, slots, lens, new_len=lens)
     want = torch.arange(B, device="cuda") + torch.minimum(accept + 1, room)
     assert torch.equal(lens.long(), want)
+
+
+# ---- a row of the batch that is idle --------------------------------------------------------------------------------
+def test_an_idle_row_does_not_trip_the_next_context(spec):
+    """Its last node is -1: its state becomes zeros, without an error that would hide a real one."""
+    B, T, V, d = 4, 3, 40, 24
+    tok, parent, nodes = i32([[1, 2, 3]] * B), i32([[-1, 0, 1]] * B), i32([3, 0, 1, 0])
+    logits = zeros(B, T, V, dtype=torch.float32)
+    logits[:, 0, 2] = logits[:, 1, 3] = 1
+    accept, last, _, _ = spec.spec_verify_tree(tok, parent, nodes, logits, n=2)
+    assert accept.tolist() == [2, 0, 0, 0] and last.tolist() == [2, -1, 0, -1]
+    state = torch.randn(B, 1, T, d, device="cuda").to(torch.bfloat16)
+    want = state[:, 0].gather(1, last.long().clamp_min(0)[:, None, None].expand(-1, 1, d))[:, 0]
+    want[1], want[3] = 0, 0
+    err = zeros(1)
+    got = spec.spec_next_ctx(state, zeros(B), last, err_workspace=err)
+    assert torch.equal(got, want) and spec.spec_poll_error(err) == spec.SPEC_OK
+    odd = torch.empty(B * T * d + 1, dtype=torch.bfloat16, device="cuda")[1:].view(B, 1, T, d)
+    odd.copy_(state)
+    given = torch.ones(B, d, dtype=torch.bfloat16, device="cuda")
+    assert spec.spec_next_ctx(odd, zeros(B), last, ctx_state=given, err_workspace=err) is given
+    assert torch.equal(given, want) and spec.spec_poll_error(err) == spec.SPEC_OK
+
+
+@pytest.mark.parametrize("best,accept", [(0, -2), (0, 3), (1, 0), (-1, 0), (-1, -1), (0, -2 ** 31)])
+def test_other_indices_out_of_range_are_still_errors(spec, best, accept):
+    err = zeros(1)
+    got = spec.spec_next_ctx(torch.ones(1, 1, 3, 8, dtype=torch.bfloat16, device="cuda"), i32([best]), i32([accept]), err_workspace=err)
+    assert (got == 0).all() and spec.spec_poll_error(err) == spec.SPEC_ERR_INDEX_RANGE
