@@ -391,7 +391,8 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
  * Limits: D a multiple of 8, at most 128; Hq a multiple of Hkv; T <= SPEC_MAX_TREE_NODES; else SPEC_ERR_SHAPE.
  * Lengths out of [0, max_pages * page_size] and node counts out of [0, T] are clamped, a page id outside [0, n_pages) reads as
  * zeros, and err_word receives SPEC_ERR_INDEX_RANGE.  A copy or a product that does not end within a second (SPEC_ERR_TIMEOUT) leaves
- * out undefined. */
+ * out and lse undefined; the call then waits for what it has asked for, once more for a second at most, and ends.  Should a copy take
+ * longer than that as well, the GPU itself is at fault, and the kernels that follow may find its bytes in their shared memory. */
 typedef struct {
     int32_t dtype, B, T, Hq, Hkv, D;
     int32_t page_size, n_pages, max_pages;

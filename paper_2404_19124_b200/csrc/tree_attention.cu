@@ -110,6 +110,7 @@ struct Shared {
     uint64_t s_full[2][2], p_full[2][2], pv_done[2][2], meet, drained, boxes_asked, rows_asked;
     uint32_t tmem_base;
     volatile int abort_flag;
+    int ended[kBoxWarps];                       // what box_role returned
     volatile int not_finite[kUnitFlags];        // the unit's tree has values that are not finite (see finite_values)
     int start_b;
     long long start_off, left;
@@ -442,8 +443,11 @@ __device__ __forceinline__ void pass_over(int n, int &slot, uint32_t &parity) {
     slot %= kSlots;
 }
 
+// Returns where the warp has ended: the slots and parities that would have been next.
+__device__ __forceinline__ int pack_end(int ks, uint32_t kp, int vs, uint32_t vp) { return ks | vs << 8 | (int)(kp << 16 | vp << 17); }
+
 template <int kHalves>
-__device__ void box_role(const AttnArgs &g, Shared *sh, uint32_t k_tiles, uint32_t v_tiles) {
+__device__ int box_role(const AttnArgs &g, Shared *sh, uint32_t k_tiles, uint32_t v_tiles) {
     using R = Ring<kHalves>;
     const int warp = (threadIdx.x >> 5) - kBoxWarp, lane = threadIdx.x & 31;
     int ks = 0, vs = 0;                                  // slots, and the parity of their `empty` that means free
@@ -462,26 +466,43 @@ __device__ void box_role(const AttnArgs &g, Shared *sh, uint32_t k_tiles, uint32
             const int now = page;
             if (t < boxed) {
                 if (t + 1 < boxed) page = box_page<kHalves>(g, u, t + 1, warp, lane);   // (ahead of the wait)
-                if (!warp_wait(&sh->k_empty[ks], kp, sh, g.a.err_word)) return;
+                if (!warp_wait(&sh->k_empty[ks], kp, sh, g.a.err_word)) return pack_end(ks, kp, vs, vp);
                 load_boxes<kHalves>(g, &g.k_map, u, t, now, warp, k_tiles + ks * R::kBytes, &sh->k_full[ks], policy);
                 pass_over<R::kK>(1, ks, kp);
             } else if (boxed < u.t1 && lane == 0) {
                 mbar_arrive(&sh->boxes_asked);
             }
             if (t > u.t0) {
-                if (!warp_wait(&sh->v_empty[vs], vp, sh, g.a.err_word)) return;
+                if (!warp_wait(&sh->v_empty[vs], vp, sh, g.a.err_word)) return pack_end(ks, kp, vs, vp);
                 load_boxes<kHalves>(g, &g.v_map, u, t - 1, before, warp, v_tiles + vs * R::kBytes, &sh->v_full[vs], policy);
                 pass_over<R::kV>(1, vs, vp);
             }
             before = now;
         }
         if (boxed < u.t1) {
-            if (!warp_wait(&sh->rows_asked, rows_parity, sh, g.a.err_word)) return;
+            if (!warp_wait(&sh->rows_asked, rows_parity, sh, g.a.err_word)) return pack_end(ks, kp, vs, vp);
             rows_parity ^= 1;
             pass_over<R::kK>(u.t1 - boxed, ks, kp);
             pass_over<R::kV>(u.t1 - boxed, vs, vp);
         }
     }
+    return pack_end(ks, kp, vs, vp);
+}
+
+// A wait has run out somewhere in the CTA: boxes that are still on their way would land in shared memory that is somebody else's by
+// then.  Whole warp, a lane per slot: the last fill that the warp knows of belongs to the round before the next one's or, in slots
+// before that one, to the same (one that was never filled is free at once).  Bounded like the other waits: a tile that some warps
+// did not come to ask for never completes its phase.
+template <int kHalves>
+__device__ void await_boxes(Shared *sh) {
+    using R = Ring<kHalves>;
+    const int lane = threadIdx.x & 31, end = sh->ended[(threadIdx.x >> 5) - kBoxWarp];
+    const bool of_k = lane < R::kK;
+    const int slot = of_k ? lane : lane - R::kK, next = of_k ? end & 0xff : end >> 8 & 0xff;
+    const uint32_t parity = (end >> (of_k ? 16 : 17) & 1) ^ (slot < next ? 1 : 0);
+    if (of_k || slot < R::kV)
+        for (const uint64_t start = now_ns(); !try_wait(of_k ? &sh->k_full[slot] : &sh->v_full[slot], parity) && now_ns() - start < kWaitMaxNs;) {}
+    __syncwarp();
 }
 
 // Rows of the tree in a tile of V.  Not every query sees them, and 0 * inf would reach those that do not: what is not finite becomes zero
@@ -1018,7 +1039,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         __syncwarp();
     } else if (warp < kBoxWarp + kBoxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBoxRegs));
-        box_role<kHalves>(g, sh, k_tiles, v_tiles);
+        const int end = box_role<kHalves>(g, sh, k_tiles, v_tiles);
+        if ((threadIdx.x & 31) == 0) sh->ended[warp - kBoxWarp] = end;
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRowRegs));
         row_role<kDtype, kHalves>(g, sh, q_tiles, k_tiles, v_tiles);
@@ -1027,6 +1049,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (sh->abort_flag) {                    // (nobody sets it any more)
+        if (warp >= kBoxWarp && warp < kBoxWarp + kBoxWarps) await_boxes<kHalves>(sh);
+        __syncthreads();
+    }
     if (warp == 8) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh->tmem_base), "r"((uint32_t)kTmemCols) : "memory");
