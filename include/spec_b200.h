@@ -410,7 +410,7 @@ size_t spec_tree_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D)
 int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* ---- spec_verify_tree: the accepted path
- * From the root on: g = first index of the maximum of the node's logits (NaN never wins); the walk goes on to the child that
+ * From the root on: g = first index of the maximum of the node's logits (a NaN counts as minus infinity); the walk goes on to the child that
  * carries token g (the lowest, if several do), and ends where there is none, or behind n of them.
  * With constraints the maximum is that of the adjusted logits of the allowed tokens, computed in fp32 in this order:
  *     x = x > 0 ? x / repetition : x * repetition   for tokens in the history or taken on the walk so far
@@ -427,10 +427,11 @@ int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace
  *   allow        dev uint32 [B, T, ceil(V / 32)], bit set: the token is allowed; NULL: all are
  *   accept_len, last_node, next_tok  dev int32 [B] (out)   tokens accepted, last node of the path, g behind it
  *   path         dev int32 [B, n + 1] (out)   nodes of the path, path[.., 0] = 0; -1 behind it
- * Limits: T <= SPEC_MAX_TREE_NODES; the tokens that penalties and biases touch have to fit a table of 200 KB per CTA, which
- * holds any for V up to 390000 (270000 with penalties and biases), and histories of 10000 tokens for V of millions; else
- * SPEC_ERR_SHAPE.  List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 (an idle row of the
- * batch) gets accept_len 0 and -1 elsewhere: spec_kv_commit leaves it as it is, spec_next_ctx writes zeros for it. */
+ * Limits: T <= SPEC_MAX_TREE_NODES.  The tokens that penalties and biases touch have to fit a table of 200 KB per CTA, of which T
+ * takes some: with penalties or biases any lists do for V up to 327680 (393216 for T <= 640), with both for V up to 196608 (262144 for T
+ * <= 768), and for V up to 2^20 lists of max_hist + max_bias + n <= 12000 entries (9000 with both); else SPEC_ERR_SHAPE.
+ * List entries outside [0, V) are ignored.  A sequence with n_nodes <= 0 (an idle row of the batch) gets accept_len 0 and -1
+ * elsewhere: spec_kv_commit leaves it as it is, spec_next_ctx writes zeros for it. */
 typedef struct {
     int32_t logits_dtype, B, T, V, n, max_hist, max_bias;
     const int32_t *tok, *parent, *n_nodes;
