@@ -214,7 +214,7 @@ int spec_verify_early(const int32_t *cand_tok, const void *base_logits, int logi
 /* ---- closing the loop (Sec. 3.1: the speculator starts from the base model's latest state vector;
  * after a verified step that is the state at the last accepted position of the best candidate) ----
  *   base_state  dev bf16 [B, K, n+1, d_base]  the base model's state vectors at the positions whose
- *                                             logits spec_verify looked at
+ *                                             logits spec_verify looked at; n >= 0 (0: a step without drafted tokens)
  *   best_cand, accept_len  dev int32 [B]      as written by spec_verify* earlier on the same stream
  *   ctx_state   dev bf16 [B, d_base] (out)    ctx_state[b,:] = base_state[b, best_cand[b], accept_len[b], :]; zeros
  *                                             where an index is out of range

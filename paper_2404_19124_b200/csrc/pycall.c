@@ -118,7 +118,7 @@ static PyObject *py_next_ctx(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     uintptr_t ps, pb, pa, px, pe = 0, st;
     int status;
     if (n != 6 || !look(a[0], t_bf16, 4, s, &ps, NULL) || !vec_i32(a[1], s[0], &pb) || !vec_i32(a[2], s[0], &pa) ||
-        !look(a[3], t_bf16, 2, x, &px, NULL) || x[0] != s[0] || x[1] != s[3] || s[2] < 2 ||
+        !look(a[3], t_bf16, 2, x, &px, NULL) || x[0] != s[0] || x[1] != s[3] ||
         !number(a[0], s_get_device, &on) || !(dev = PyObject_CallNoArgs(get_device)))
         return unusual();
     const int here = PyLong_AsLongLong(dev) == on;   /* the tensors' device is current */

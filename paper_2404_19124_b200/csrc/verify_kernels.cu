@@ -745,7 +745,7 @@ extern "C" int spec_next_ctx(const void *base_state, const int32_t *best_cand, c
                              int n, int d_base, void *ctx_state, int32_t *err_word, void *cuda_stream) {
     using namespace spec;
     if (!base_state || !best_cand || !accept_len || !ctx_state) return SPEC_ERR_INVALID_ARG;
-    if (B <= 0 || K <= 0 || n <= 0 || d_base <= 0) return SPEC_ERR_INVALID_ARG;
+    if (B <= 0 || K <= 0 || n < 0 || d_base <= 0) return SPEC_ERR_INVALID_ARG;
     if (((uintptr_t)base_state % 2) != 0 || ((uintptr_t)ctx_state % 2) != 0) return SPEC_ERR_INVALID_ARG;
     if (err_word && ((uintptr_t)err_word % 4) != 0) return SPEC_ERR_INVALID_ARG;
     const int vec_ok = (d_base % 8 == 0) && ((uintptr_t)base_state % 16) == 0 && ((uintptr_t)ctx_state % 16) == 0;
