@@ -410,8 +410,8 @@ size_t spec_tree_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D)
 int spec_tree_attention(const spec_tree_attention_t *a /*host*/, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* ---- spec_verify_tree: the accepted path
- * From the root on: g = first index of the maximum of the node's logits (a NaN counts as minus infinity); the walk goes on to the child that
- * carries token g (the lowest, if several do), and ends where there is none, or behind n of them.
+ * From the root on: g = first index of the maximum of the node's logits (a NaN counts as minus infinity); the walk goes on to the
+ * child that carries token g (the lowest, if several do), and ends where there is none, or behind n of them.
  * With constraints the maximum is that of the adjusted logits of the allowed tokens, computed in fp32 in this order:
  *     x = x > 0 ? x / repetition : x * repetition   for tokens in the history or taken on the walk so far
  *     x = x - frequency * c - presence              for tokens generated c > 0 times: in the history behind the prompt, or on the walk

@@ -24,10 +24,10 @@
 // busy, nor the exponentials, 39 %, were the limit, but the way round.)  Units of more than 128 rows have a stream per 128
 // rows, which take both halves of every tile of keys; in smaller ones each stream takes a half, and the two results are joined.
 //
-// What bounds it.  Up to 128 rows per key head, the keys' way from HBM: 131072 tokens of one sequence 113 to 120 us, 4.6 TB/s of
-// 6.5; 16 sequences with 40 key heads and trees of 31 to 61 nodes 111 to 120 us, 3.6 TB/s (units of 10 tiles, whose ends nothing hides).
+// What bounds it.  Up to 128 rows per key head, the keys' way from HBM: 131072 tokens of one sequence 110 to 120 us, 4.6 TB/s of
+// 6.5; 16 sequences with 40 key heads and trees of 31 to 61 nodes 110 to 120 us, 3.6 TB/s (units of 10 tiles, whose ends nothing hides).
 // With more rows the chain scores - softmax - products of a step and the power cap: 64 sequences, trees of 65 to 129 nodes,
-// four query heads per key head 368 us from a cool start, 400 to 460 on and on (1.6 GHz), 0.55 of 1.63 PFLOP/s.  Few tiles:
+// four query heads per key head 368 us from a cool start, 390 to 460 on and on (1.6 GHz), 0.55 of 1.63 PFLOP/s.  Few tiles:
 // latency, 20 us for single tokens of 4 sequences, of which the second kernel is 4.
 #include <limits.h>
 #include <math.h>
@@ -90,6 +90,10 @@ constexpr int kMaxK = 6, kMaxV = 5;
 // The cost of the whole call is dealt to `ctas` CTAs: CTA c has the tiles that begin in [start(c), start(c + 1)).  A unit costs
 // unit_cost beside its tiles, behind its first one: what its end takes (a masked tile, results, a pipeline that empties) is time that
 // no tile explains.  CTAs are as few as it takes for each to have a tile in every unit that its run meets.
+// Costs of 0, 2, 3 and 4, us: 13B trees 135, 115, 110, 109; trees of 65 to 129 nodes, grouped heads, 447, 432, 393, 405; 32 short
+// sequences of 40 heads 180, 130, 129, 127; 64 chains of 4 tokens, grouped heads, 133, 123, 125, 127; 256 single tokens 304, 274,
+// 270, 270; one long context 112, 111, 111, 111.  With fewer than kManyTiles tiles a CTA it makes no difference (single
+// tokens of 4 sequences 20.8 either way, 8 trees of 33 nodes 35.8 and 35.7).
 constexpr int kUnitCost = 3;           // where CTAs have at least kManyTiles of cost each, else 0
 constexpr int kManyTiles = 16;
 struct Deal {
@@ -501,7 +505,8 @@ __device__ void await_boxes(Shared *sh) {
     const int slot = of_k ? lane : lane - R::kK, next = of_k ? end & 0xff : end >> 8 & 0xff;
     const uint32_t parity = (end >> (of_k ? 16 : 17) & 1) ^ (slot < next ? 1 : 0);
     if (of_k || slot < R::kV)
-        for (const uint64_t start = now_ns(); !try_wait(of_k ? &sh->k_full[slot] : &sh->v_full[slot], parity) && now_ns() - start < kWaitMaxNs;) {}
+        for (const uint64_t start = now_ns();
+             !try_wait(of_k ? &sh->k_full[slot] : &sh->v_full[slot], parity) && now_ns() - start < kWaitMaxNs;) {}
     __syncwarp();
 }
 
@@ -1140,6 +1145,9 @@ size_t join_bytes() { return aligned((size_t)num_sms() * sizeof(Join)); }
 
 // The cache as a TMA tensor whose boxes are a page, or 128 tokens of one, by 64 columns of a head.  Pages have to tile 128 keys
 // or be tiled by them, in whole groups of 8 rows (the swizzle's period).  False: not such a cache, or strides that TMA does not take.
+// By TMA and row by row, us: 131072 tokens 111 to 121, four sequences of 20000 to 40000 100 to 107, 13B trees with pages of 8, 16 and 128
+// 110, 110, 106 to 112 each, 64 chains of 4 tokens, grouped heads, 125 to 134, trees of 65 to 129 nodes 393 to 414; short units, where
+// the first tile's way counts, are the exception: 32 sequences of 100 to 700 tokens 129 to 121, heads of 64 46.5 to 45.3.
 bool cache_map(const spec_tree_attention_t &a, const void *base, const int64_t (&stride)[3], int box_tokens, CUtensorMap *map) {
     static const auto encode = []() -> decltype(&cuTensorMapEncodeTiled) {
         void *fn = nullptr;

@@ -44,7 +44,7 @@ __device__ int block_inclusive_sum(int x, int *part, int &total) {
 // One CTA per sequence.  Level by level, candidates with the same first j + 1 tokens find each other through a hash table in
 // shared memory whose entries keep the lowest of them (a table of pairs (lowest candidate with the same j tokens, token)); an entry
 // (k, j) whose lowest candidate is k itself is a new node, and its number is its rank in (k, j) order, a prefix sum.
-// All of it is latency: 2 n + 6 barriers.
+// All of it is latency: 3 n + 5 barriers.
 constexpr int kPlanMaxThreads = 1024;
 
 struct PlanSmem {            // offsets in bytes
@@ -161,7 +161,10 @@ tree_plan_kernel(const int32_t *cand, const int32_t *last_tok, const int32_t *se
 
 // ---- block tables and slots ----------------------------------------------------------------------------------------
 // The prefix sum that deals the free pages needs all sequences, so one CTA grows the tables; it writes the slots too while
-// they are few, otherwise a second kernel does with the whole GPU.
+// they are few, otherwise a second kernel does with the whole GPU.  One kernel against two, us on the device: 64 sequences of 32, 64, 96
+// and 128 slots 5.3 to 6.9, 6.2 to 6.9, 7.2 to 7.0, 8.4 to 7.0; one sequence of 4096 and 6144 6.3 to 6.8, 8.0 to 7.1; 1024 of 1 and 4
+// 7.7 to 8.5, 11.3 to 10.0.
+constexpr int kOneKernelSlots = 4096;
 constexpr int kTableThreads = 1024;
 constexpr int kSlotThreads = 256;
 
@@ -349,7 +352,7 @@ struct Best {
     float value;
     int tok;
     __device__ __forceinline__ void offer(float x, int t) {
-        x = x != x ? -INFINITY : x;          // a NaN never wins
+        x = x != x ? -INFINITY : x;          // a NaN counts as minus infinity
         if (x > value || (x == value && t < tok)) {
             value = x;
             tok = t;
@@ -794,7 +797,7 @@ int spec_page_tables(const int32_t *seq_len, const int32_t *n_new, int B, int pa
                          free_count, n_free, slots, n_pages_out, free_count_out, err_word};
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const int all = B * max_new;
-    const bool one = all <= 4 * kTableThreads;
+    const bool one = all <= kOneKernelSlots;
     SPEC_CUDA_TRY(launch_pdl(page_tables_kernel, dim3(1), dim3(kTableThreads), 0, st, a, one ? 1 : 0));
     if (!one) {
         const int blocks = (all - 1) / kSlotThreads + 1, most = 8 * num_sms();
